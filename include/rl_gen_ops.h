@@ -216,6 +216,101 @@ int rl_op_sample(const float *logits, int32_t B, int32_t V, float temperature, c
 int rl_op_logprob_gather(const float *logits, int64_t ld, int32_t M, int32_t V, const int32_t *tokens, int32_t T,
                          int64_t m_first, float *out, void *hip_stream);
 
+/* ---- Steps of several tokens over a bounded cache --------------------------------------------------------------------
+ * A decode step may feed each sequence several tokens at once (tokens drafted by a smaller model or a table, of which the
+ * target keeps a prefix), and a cache may be held to a fixed number of rows per kv head.  The five calls below are the steps
+ * of such a program for one layer's cache: append the new rows, attend, verify the drafts, evict.  Once rows have been evicted
+ * the slot of a row in the cache is no longer its position in the text, so both are given.
+ *
+ * Shared arguments.  A span is the T new tokens of a sequence; token t of sequence b is row m = b * T + t of the activations.
+ * d_span (DEVICE int32 [B] or NULL): sequence b has only clamp(d_span[b], 0, T) new tokens, NULL: T; the rows of the others are
+ * not read as queries and their outputs are left as they were.  kc / vc: the cache rows of one layer, IEEE half or, with
+ * kscale / vscale, block-scaled.  table (DEVICE int32 [B, table_stride] or NULL): the cache is a pool of pages
+ * [n_pages][Hkv][page_size][hd] as in rl_op_decode_attention_paged (entries of rows in use must name pages of the pool, they are
+ * not checked; page_size a power of two in [16, 4096], table_stride * page_size >= S); NULL: slabs [B][Hkv][S][hd], page_size and
+ * table_stride without effect.  hd is 64 or 128.  weight (fp32) and row_pos / pos (int32) are [B][Hkv][S] arrays beside the cache,
+ * indexed by slot whether the cache is paged or not.  Device pointers of q, out, kc, vc and qkv are 16-byte aligned (E_SHAPE
+ * otherwise), all others by their element. */
+
+/* Rotary table with the frequencies scaled for contexts longer than the model was trained on: tab fp32 [n_pos, rot_dim/2, 2] =
+ * (cos, sin) of pos * f_r, f_r evaluated in fp64 on the host and copied (synchronously).  rot_dim is the number of leading head
+ * elements that rotate (rot_dim % 2 == 0).  With f0_r = base^(-2r/rot_dim):
+ *   kind 0  f_r = f0_r (rl_op_build_rope_table's values; factor and orig_len without effect)
+ *   kind 1  linear: f_r = f0_r / factor
+ *   kind 2  base: the base is replaced by base * factor^(rot_dim/(rot_dim-2)), so that the slowest pair slows down by factor and the
+ *           fastest not at all (rot_dim > 2)
+ *   kind 3  by parts: a pair that turns more than high times over orig_len positions keeps f0_r, one that turns less than low
+ *           times is slowed by factor, in between the two are blended linearly in the number of turns (0 < low < high)
+ * factor >= 1, base > 0; n_pos >= 1. */
+int rl_op_build_rope_table_scaled(float *tab, int32_t n_pos, int32_t rot_dim, float base, int32_t kind, float factor, int32_t orig_len,
+                                  float low, float high);
+
+/* Rotary embedding and append of a span at given positions and slots.  qkv fp32: nsplit partials, each [B*T, (Hq+2Hkv)*hd] laid out
+ * q | k | v per row, split_stride elements apart (a multiple of 4).  Row (b, t) is at position d_pos[b] + t and goes to slot
+ * d_slot[b] + t (DEVICE int32 [B] each).  The first rot_dim elements of every q and k head are rotated with rope_tab (fp32 [tab_rows, rot_dim/2, 2]):
+ * style 0 turns elements (2r, 2r+1), style 1 elements (r, r + rot_dim/2); the others are copied.  rot_dim % 8 == 0, 8 <= rot_dim <= hd.
+ * q goes to q_f32 and / or q_f16 (+ q_f16_lo, its second half term), each [B*T, Hq*hd] or NULL; k and v become cache rows.
+ * weight and row_pos (either may be NULL): the entry of every new row is set to 0 and to its position.
+ * A row whose position is outside [0, tab_rows) or whose slot is outside [0, S) is skipped whole. */
+int rl_op_rope_append_at(const float *qkv, int32_t nsplit, size_t split_stride, int32_t B, int32_t T, const int32_t *d_pos,
+                         const int32_t *d_slot, const int32_t *d_span, const float *rope_tab, int32_t tab_rows, int32_t rope_style,
+                         int32_t rot_dim, int32_t Hq, int32_t Hkv, int32_t hd, int32_t S, float *q_f32, uint16_t *q_f16, uint16_t *q_f16_lo,
+                         uint16_t *kc, uint16_t *vc, float *kscale, float *vscale, const int32_t *table, int32_t table_stride,
+                         int32_t page_size, float *weight, int32_t *row_pos, void *hip_stream);
+
+/* Attention of a span over the cache: query (b, t) of head u sees the cache rows 0 .. d_len[b] + t of kv head u / (Hq/Hkv) -- the
+ * rows that were there (d_len[b] of them, DEVICE int32 [B], clamped to [0, S]) and the span's own up to itself, which the caller has
+ * stored at slots d_len[b] .. -- and never more than S rows.  out[b, t] = sum_j p_j v_j, p = softmax_j(q . k_j / sqrt(hd)).
+ * q fp32 [B*T, Hq*hd], rotated; out f16 [B*T, Hq*hd], out_lo its second half term or NULL.  T = 1 is decode attention.
+ * weight (or NULL): weight[b, h, j] += the sum of p_j over the queries of kv head h and the span's valid tokens -- what
+ * rl_op_evict_rows goes by.  Sums are formed in a fixed order (the same bits every time), also those of weight.
+ * nsplit: workgroups that share the rows of a sequence, 1 .. 64, or 0: chosen from the shape.  ws fp32
+ * [rl_op_span_attention_ws_floats(same arguments, weights = whether weight is given)] (may be NULL when that is 0), 16-byte aligned.
+ * A query sees a row whose K or V is not finite as a non-finite score or value; rows that a query does not see never reach
+ * its result, whatever they hold.  Hq/Hkv <= 64. */
+int rl_op_span_attention(const float *q, const uint16_t *kc, const uint16_t *vc, const float *kscale, const float *vscale,
+                         const int32_t *table, int32_t table_stride, int32_t page_size, const int32_t *d_len, const int32_t *d_span,
+                         uint16_t *out, uint16_t *out_lo, float *weight, float *ws, int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd,
+                         int32_t S, int32_t nsplit, void *hip_stream);
+size_t rl_op_span_attention_ws_floats(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, int32_t S, int32_t nsplit,
+                                      int32_t weights);
+
+/* Eviction by accumulated attention weight: of the n = d_len[b] (clamped to [0, S]) cache rows of a sequence and kv head, at most
+ * `keep` stay: the `recent` newest and, of the others, those with the largest weight (ties and, after them, NaN -- which counts as
+ * minus infinity -- to the lowest slot).  Newest goes by pos: rows with pos > max(pos) - recent; with pos == NULL by slot, the
+ * last `recent`.  Rows of kv heads are chosen independently.  Nothing moves when n <= keep.  Otherwise the rows that stay and
+ * already lie below slot `keep` are not touched, and the j-th free slot below `keep` (ascending) receives the j-th staying row at or
+ * above it (ascending): K and V rows and their scales, in place.  weight_out / pos_out: the values of the rows now in slots
+ * 0 .. min(n, keep) - 1, entries behind are left as they were; each may be the array it is taken from (pos_out is required with pos).
+ * d_len_out (DEVICE int32 [B], may be d_len, or NULL): min(n, keep).  1 <= keep <= S, 0 <= recent <= keep.
+ * ws: DEVICE, rl_op_evict_rows_ws_bytes bytes, 8-byte aligned. */
+int rl_op_evict_rows(uint16_t *kc, uint16_t *vc, float *kscale, float *vscale, const int32_t *table, int32_t table_stride,
+                     int32_t page_size, const float *weight, float *weight_out, const int32_t *pos, int32_t *pos_out, const int32_t *d_len,
+                     int32_t *d_len_out, void *ws, int32_t B, int32_t Hkv, int32_t hd, int32_t S, int32_t keep, int32_t recent,
+                     void *hip_stream);
+size_t rl_op_evict_rows_ws_bytes(int32_t B, int32_t Hkv, int32_t S, int32_t keep);
+
+/* Verification of drafted tokens with given random numbers, so that the tokens that come out are distributed as the target model's own.
+ * target fp32 [B*(T+1), V] (row stride ldt >= V): row b*(T+1)+i holds the target's logits after i drafted tokens of sequence b; draft fp32
+ * [B*T, V] (row stride ldd >= V): the logits that drafted token i was sampled from, NULL: the drafts were not sampled (q puts all weight on the
+ * drafted token); drafts int32 [B, T]; u fp32 [B, T+1] in [0, 1).
+ * temperature > 0: p_i = softmax(target_i / temperature), q_i likewise from draft; drafted token x_i is accepted while u[b,i] * q_i(x_i) <
+ * p_i(x_i), up to the first that is not (ids outside [0, V) never are).  The next token is then drawn by inversion with u[b,T]
+ * -- the smallest v whose cumulative weight exceeds u times the total -- from max(0, p_i - q_i) at the rejected position (from p_i where that is
+ * zero everywhere), or from p_n when all n = clamp(d_span[b], 0, T) drafts were accepted.
+ * temperature <= 0: greedy, drafted token i is accepted while it is the lowest index of the largest target logit, which is
+ * also the next token (draft and u may be NULL and are not read).
+ * accepted int32 [B]; tokens int32 [B, T+1]: the accepted tokens, the next token, then -1.  A target or draft row that is
+ * reached and holds a NaN (temperature > 0: or no finite largest value) ends the sequence's acceptance, and its next token is -1.
+ * logp fp32 [B, T+1] or NULL: log p of each token of `tokens` under the target row it follows (temperature <= 0: at temperature 1, and
+ * NaN where that row's largest logit is not finite), 0 for -1.
+ * Weights and sums are formed in fp64 from the fp32 logits (relative error below 1e-11), in a fixed order.  1 <= T <= 256.
+ * ws: DEVICE, rl_op_verify_drafts_ws_bytes bytes, 8-byte aligned. */
+int rl_op_verify_drafts(const float *target, int64_t ldt, const float *draft, int64_t ldd, const int32_t *drafts, const float *u,
+                        const int32_t *d_span, int32_t B, int32_t T, int32_t V, double temperature, int32_t *accepted, int32_t *tokens,
+                        float *logp, void *ws, void *hip_stream);
+size_t rl_op_verify_drafts_ws_bytes(int32_t B, int32_t T, int32_t V);
+
 /* Plain device-to-device copy of `bytes` bytes (multiple of 16; 16-byte aligned pointers), 16 bytes per
  * lane.  Not a step of the method: a kernel of exactly known traffic that the benchmark profiles next
  * to the real kernels to scale hardware byte counters. */

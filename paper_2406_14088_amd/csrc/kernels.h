@@ -186,3 +186,67 @@ bool decode_attention_shares_items(int B, int Hq, int Hkv, int S, int nsplit);
 void launch_prefill_attention(const f16_t *q, const f16_t *kc, const f16_t *vc, f16_t *out, int nb, int b0, int T,
                               int Hq, int Hkv, int hd, int S, hipStream_t st, KvMap map = KvMap(),
                               const int32_t *d_valid = nullptr, f16_t *out_lo = nullptr, const f16_t *q_lo = nullptr);
+
+// ---- rope_append_at.hip, attention_span.hip, cache_evict.hip, verify_drafts.hip: steps of several tokens over a bounded cache ----
+// (the operations and the meaning of every argument: rl_gen_ops.h; sizes are checked by the entry points)
+struct RopeAppendAtArgs {
+    const float *qkv;
+    int nsplit;
+    size_t split_stride;
+    int B, T;
+    const int32_t *d_pos, *d_slot, *d_span;
+    const float *rope_tab;
+    int tab_rows, rope_style, rot_dim, Hq, Hkv, hd, S;
+    float *q_f32;
+    f16_t *q_f16, *q_f16_lo, *kc, *vc;
+    KvMap map;
+    float *weight;
+    int32_t *row_pos;
+};
+void launch_rope_append_at(const RopeAppendAtArgs &a, hipStream_t st);
+
+struct SpanArgs {
+    const float *q;
+    const f16_t *kc, *vc;
+    KvMap map;
+    const int32_t *d_len, *d_span;
+    f16_t *out, *out_lo;
+    float *weight, *ws;
+    int B, T, Hq, Hkv, hd, S, nsplit;
+};
+int span_attention_splits(int B, int T, int Hq, int Hkv, int hd, int S);  // what nsplit = 0 resolves to
+size_t span_attention_ws_floats(int B, int T, int Hq, int Hkv, int hd, int S, int nsplit, bool weights);
+void launch_span_attention(const SpanArgs &a, hipStream_t st);
+
+struct EvictArgs {
+    f16_t *kc, *vc;
+    KvMap map;
+    const float *weight;
+    float *weight_out;
+    const int32_t *pos;
+    int32_t *pos_out;
+    const int32_t *d_len;
+    int32_t *d_len_out;
+    int32_t *moves;      // workspace
+    int max_moves;       // set by the launcher
+    int B, Hkv, hd, S, keep, recent;
+};
+size_t evict_rows_ws_bytes(int B, int Hkv, int S, int keep);
+void launch_evict_rows(const EvictArgs &a, hipStream_t st);
+
+struct VerifyArgs {
+    const float *target;
+    int64_t ldt;
+    const float *draft;
+    int64_t ldd;
+    const int32_t *drafts;
+    const float *u;
+    const int32_t *d_span;
+    int B, T, V;
+    double temperature;
+    int32_t *accepted, *tokens;
+    float *logp;
+    void *ws;
+};
+size_t verify_drafts_ws_bytes(int B, int T, int V);
+void launch_verify_drafts(const VerifyArgs &a, hipStream_t st);

@@ -6,6 +6,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <exception>
 #include <mutex>
 #include <vector>
 
@@ -1694,6 +1695,146 @@ int rl_op_logprob_gather(const float *logits, int64_t ld, int32_t M, int32_t V, 
     if (!logits || !tokens || !out) return RL_GEN_E_NULL;
     if (M < 0 || V <= 0 || ld < V || T <= 0 || m_first < 0) return RL_GEN_E_SHAPE;
     launch_logprob_gather(logits, ld, M, V, tokens, T, m_first, out, reinterpret_cast<hipStream_t>(st));
+    RL_OP_RETURN();
+}
+
+// ---- steps of several tokens over a bounded cache
+
+// Fills `map` from the cache arguments that these calls share; RL_GEN_E_NULL / RL_GEN_E_SHAPE when they do not fit together.
+static int span_cache_map(const void *kc, const void *vc, const float *kscale, const float *vscale, const int32_t *table, int32_t table_stride,
+                          int32_t page_size, int32_t B, int32_t Hkv, int32_t hd, int32_t S, KvMap *map) {
+    if (!kc || !vc || (kscale == nullptr) != (vscale == nullptr)) return RL_GEN_E_NULL;
+    if (B < 0 || Hkv <= 0 || (hd != 64 && hd != 128) || S <= 0 || (int64_t)B * Hkv > INT32_MAX / 64) return RL_GEN_E_SHAPE;
+    if (((uintptr_t)kc | (uintptr_t)vc) % 16) return RL_GEN_E_SHAPE;
+    map->kscale = const_cast<float *>(kscale); map->vscale = const_cast<float *>(vscale);
+    if (table) {
+        const int shift = page_shift_of(page_size);
+        if (!shift || table_stride <= 0 || (int64_t)table_stride * page_size < S) return RL_GEN_E_SHAPE;
+        map->table = table; map->table_stride = table_stride; map->page_shift = shift;
+    }
+    return RL_GEN_OK;
+}
+
+int rl_op_build_rope_table_scaled(float *tab, int32_t n_pos, int32_t rot_dim, float base, int32_t kind, float factor, int32_t orig_len,
+                                  float low, float high) {
+    if (!tab) return RL_GEN_E_NULL;
+    if (n_pos <= 0 || rot_dim <= 0 || rot_dim % 2 || rot_dim > 65536 || !(base > 0.f) || base > 3e38f || kind < 0 || kind > 3) return RL_GEN_E_SHAPE;
+    if (kind != 0 && (!(factor >= 1.f) || factor > 3e38f)) return RL_GEN_E_SHAPE;
+    if (kind == 2 && rot_dim <= 2) return RL_GEN_E_SHAPE;
+    if (kind == 3 && (orig_len <= 0 || !(low > 0.f) || !(high > low) || high > 3e38f)) return RL_GEN_E_SHAPE;
+    try {
+        const int half = rot_dim / 2;
+        std::vector<double> freq(half);
+        const double b = kind == 2 ? (double)base * pow((double)factor, rot_dim / (rot_dim - 2.0)) : (double)base;
+        for (int r = 0; r < half; ++r) {
+            const double f0 = pow(b, -2.0 * r / (double)rot_dim);
+            freq[r] = f0;
+            if (kind == 1) freq[r] = f0 / factor;
+            if (kind == 3) {  // turns of the pair over the original length decide how much of the slow-down it takes
+                const double turns = orig_len * f0 / 6.283185307179586476925;
+                const double keep = turns >= high ? 1.0 : turns <= low ? 0.0 : (turns - low) / ((double)high - low);
+                freq[r] = keep * f0 + (1.0 - keep) * f0 / factor;
+            }
+        }
+        std::vector<float> t((size_t)n_pos * rot_dim);
+        for (int pos = 0; pos < n_pos; ++pos)
+            for (int r = 0; r < half; ++r) {
+                const double ang = (double)pos * freq[r];
+                t[((size_t)pos * half + r) * 2] = (float)cos(ang);
+                t[((size_t)pos * half + r) * 2 + 1] = (float)sin(ang);
+            }
+        return hipMemcpy(tab, t.data(), t.size() * sizeof(float), hipMemcpyHostToDevice) == hipSuccess ? RL_GEN_OK : RL_GEN_E_HIP;
+    } catch (const std::exception &) {  // out of host memory
+        set_err(nullptr, "rl_op_build_rope_table_scaled: no host memory for %d positions", n_pos);
+        return RL_GEN_E_CAPACITY;
+    }
+}
+
+int rl_op_rope_append_at(const float *qkv, int32_t nsplit, size_t split_stride, int32_t B, int32_t T, const int32_t *d_pos,
+                         const int32_t *d_slot, const int32_t *d_span, const float *rope_tab, int32_t tab_rows, int32_t rope_style,
+                         int32_t rot_dim, int32_t Hq, int32_t Hkv, int32_t hd, int32_t S, float *q_f32, uint16_t *q_f16, uint16_t *q_f16_lo,
+                         uint16_t *kc, uint16_t *vc, float *kscale, float *vscale, const int32_t *table, int32_t table_stride,
+                         int32_t page_size, float *weight, int32_t *row_pos, void *st) {
+    if (!qkv || !d_pos || !d_slot || !rope_tab || (q_f16_lo && !q_f16)) return RL_GEN_E_NULL;
+    RopeAppendAtArgs a;
+    if (int rc = span_cache_map(kc, vc, kscale, vscale, table, table_stride, page_size, B, Hkv, hd, S, &a.map)) return rc;
+    if (nsplit < 1 || split_stride % 4 || T <= 0 || (int64_t)B * T > INT32_MAX || tab_rows <= 0 || (rope_style != 0 && rope_style != 1) ||
+        rot_dim < 8 || rot_dim > hd || rot_dim % 8 || Hq <= 0 || (int64_t)Hq + 2 * (int64_t)Hkv > 65535)
+        return RL_GEN_E_SHAPE;
+    if (((uintptr_t)qkv | (uintptr_t)q_f32 | (uintptr_t)q_f16 | (uintptr_t)q_f16_lo | (uintptr_t)rope_tab) % 16) return RL_GEN_E_SHAPE;
+    a.qkv = qkv; a.nsplit = nsplit; a.split_stride = split_stride; a.B = B; a.T = T;
+    a.d_pos = d_pos; a.d_slot = d_slot; a.d_span = d_span;
+    a.rope_tab = rope_tab; a.tab_rows = tab_rows; a.rope_style = rope_style; a.rot_dim = rot_dim;
+    a.Hq = Hq; a.Hkv = Hkv; a.hd = hd; a.S = S;
+    a.q_f32 = q_f32; a.q_f16 = q_f16; a.q_f16_lo = q_f16_lo; a.kc = kc; a.vc = vc;
+    a.weight = weight; a.row_pos = row_pos;
+    launch_rope_append_at(a, reinterpret_cast<hipStream_t>(st));
+    RL_OP_RETURN();
+}
+
+static bool span_shape_ok(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, int32_t S, int32_t nsplit) {
+    return B >= 0 && T > 0 && T <= S && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Hq / Hkv <= 64 && (hd == 64 || hd == 128) && nsplit >= 0 &&
+           nsplit <= 64 && (int64_t)B * T * Hq <= INT32_MAX / 64;
+}
+
+size_t rl_op_span_attention_ws_floats(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, int32_t S, int32_t nsplit, int32_t weights) {
+    if (!span_shape_ok(B, T, Hq, Hkv, hd, S, nsplit)) return 0;
+    return span_attention_ws_floats(B, T, Hq, Hkv, hd, S, nsplit ? nsplit : span_attention_splits(B, T, Hq, Hkv, hd, S), weights != 0);
+}
+
+int rl_op_span_attention(const float *q, const uint16_t *kc, const uint16_t *vc, const float *kscale, const float *vscale,
+                         const int32_t *table, int32_t table_stride, int32_t page_size, const int32_t *d_len, const int32_t *d_span,
+                         uint16_t *out, uint16_t *out_lo, float *weight, float *ws, int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd,
+                         int32_t S, int32_t nsplit, void *st) {
+    if (!q || !d_len || !out) return RL_GEN_E_NULL;
+    SpanArgs a;
+    if (int rc = span_cache_map(kc, vc, kscale, vscale, table, table_stride, page_size, B, Hkv, hd, S, &a.map)) return rc;
+    if (!span_shape_ok(B, T, Hq, Hkv, hd, S, nsplit)) return RL_GEN_E_SHAPE;
+    if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)out_lo | (uintptr_t)ws) % 16) return RL_GEN_E_SHAPE;
+    a.nsplit = nsplit ? nsplit : span_attention_splits(B, T, Hq, Hkv, hd, S);
+    if (!ws && span_attention_ws_floats(B, T, Hq, Hkv, hd, S, a.nsplit, weight != nullptr) > 0) return RL_GEN_E_NULL;
+    a.q = q; a.kc = kc; a.vc = vc; a.d_len = d_len; a.d_span = d_span; a.out = out; a.out_lo = out_lo; a.weight = weight; a.ws = ws;
+    a.B = B; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.hd = hd; a.S = S;
+    launch_span_attention(a, reinterpret_cast<hipStream_t>(st));
+    RL_OP_RETURN();
+}
+
+size_t rl_op_evict_rows_ws_bytes(int32_t B, int32_t Hkv, int32_t S, int32_t keep) {
+    if (B < 0 || Hkv <= 0 || S <= 0 || keep < 1 || keep > S) return 0;
+    return evict_rows_ws_bytes(B, Hkv, S, keep);
+}
+
+int rl_op_evict_rows(uint16_t *kc, uint16_t *vc, float *kscale, float *vscale, const int32_t *table, int32_t table_stride,
+                     int32_t page_size, const float *weight, float *weight_out, const int32_t *pos, int32_t *pos_out, const int32_t *d_len,
+                     int32_t *d_len_out, void *ws, int32_t B, int32_t Hkv, int32_t hd, int32_t S, int32_t keep, int32_t recent, void *st) {
+    if (!weight || !weight_out || (pos && !pos_out) || !d_len || !ws) return RL_GEN_E_NULL;
+    EvictArgs a;
+    if (int rc = span_cache_map(kc, vc, kscale, vscale, table, table_stride, page_size, B, Hkv, hd, S, &a.map)) return rc;
+    if (keep < 1 || keep > S || recent < 0 || recent > keep || (uintptr_t)ws % 8) return RL_GEN_E_SHAPE;
+    a.kc = kc; a.vc = vc; a.weight = weight; a.weight_out = weight_out; a.pos = pos; a.pos_out = pos ? pos_out : nullptr;
+    a.d_len = d_len; a.d_len_out = d_len_out; a.moves = reinterpret_cast<int32_t *>(ws);
+    a.B = B; a.Hkv = Hkv; a.hd = hd; a.S = S; a.keep = keep; a.recent = recent; a.max_moves = 0;
+    launch_evict_rows(a, reinterpret_cast<hipStream_t>(st));
+    RL_OP_RETURN();
+}
+
+static bool verify_shape_ok(int32_t B, int32_t T, int32_t V) {
+    return B >= 0 && T >= 1 && T <= 256 && V > 0 && (int64_t)B * (2 * (int64_t)T + 1) <= INT32_MAX / 1024;
+}
+
+size_t rl_op_verify_drafts_ws_bytes(int32_t B, int32_t T, int32_t V) { return verify_shape_ok(B, T, V) ? verify_drafts_ws_bytes(B, T, V) : 0; }
+
+int rl_op_verify_drafts(const float *target, int64_t ldt, const float *draft, int64_t ldd, const int32_t *drafts, const float *u,
+                        const int32_t *d_span, int32_t B, int32_t T, int32_t V, double temperature, int32_t *accepted, int32_t *tokens,
+                        float *logp, void *ws, void *st) {
+    const bool sampled = temperature > 0;
+    if (!target || !drafts || !accepted || !tokens || !ws || (sampled && !u)) return RL_GEN_E_NULL;
+    if (!verify_shape_ok(B, T, V) || ldt < V || (sampled && draft && ldd < V) || (uintptr_t)ws % 8) return RL_GEN_E_SHAPE;
+    if (temperature != temperature || temperature > 1e300 || (sampled && temperature < 1e-30)) return RL_GEN_E_SHAPE;
+    VerifyArgs a;
+    a.target = target; a.ldt = ldt; a.draft = sampled ? draft : nullptr; a.ldd = ldd; a.drafts = drafts; a.u = u; a.d_span = d_span;
+    a.B = B; a.T = T; a.V = V; a.temperature = temperature; a.accepted = accepted; a.tokens = tokens; a.logp = logp; a.ws = ws;
+    launch_verify_drafts(a, reinterpret_cast<hipStream_t>(st));
     RL_OP_RETURN();
 }
 
