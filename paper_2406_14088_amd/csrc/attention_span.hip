@@ -1,73 +1,616 @@
 // Attention of a span of new tokens over a cache (rl_op_span_attention), with the attention weight of every cached row on request.
+//
+// The T tokens of a sequence and the G = Hq / Hkv query heads of a kv head are R = T * G query rows that share every cache row: per tile
+// of 32 cache rows two matrix products,
+//     S^T[32 keys x 16 columns] = K[32 x hd] * Q^T[hd x 16],     O^T[hd x 16 columns] += V^T[hd x 32 keys] * P^T[32 x 16],
+// where 16 columns are the high and the low half term of 8 query rows (columns c and c + 8): q and the probabilities enter the
+// matrix cores with about 22 significant bits, K and V as stored (a block-scaled int16 n as the exact sum of the two halves
+// n & ~31 and n & 31).  A wavefront takes NT = 1, 2 or 4 such column tiles (8, 16 or 32 query rows); more rows are further workgroups
+// that find the cache rows in the L2 of their XCD.  S^T leaves a lane with 4 keys of a column per 16-key product, which is the
+// layout that P^T needs: key 4 j + i of the first 16 keys is contraction index 8 j + i, of the second 8 j + 4 + i.
+//
+// One pass with a running maximum and sum per query row.  The maximum is raised (and the accumulators rescaled) only when a score
+// exceeds it by more than 2^8, so that most tiles need no reduction across lanes: weights up to 2^8 are as exact in two half terms as
+// weights up to 1.  Scores are kept in units of log 2 (q is scaled by log2(e) / sqrt(hd) before it is split).
+//
+// Memory: each wavefront copies its K and V tiles from HBM into its own LDS ring (buffer loads with the LDS destination, 16 rows per
+// buffer descriptor: pages hold a multiple of 16 rows; rows past the end arrive as zeros), so no barrier is needed in the loop.  16-byte
+// pieces are stored XOR-permuted: K operands (one row per lane) and V operands (transposed by the LDS read) are free of bank conflicts.
+// W = 1, 2 or 4 wavefronts share the rows of a sequence and join through LDS at the end; nsplit workgroups join in a second
+// kernel, which also turns the scores kept in the workspace into weights.
 #include "kernels.h"
 
-__device__ __forceinline__ float span_elem(const f16_t *row, int e, const float *scale, size_t rowi) {
-    return scale ? (float)(int16_t)row[e] * scale[rowi] : f16_to_f32(row[e]);
+#define SPAN_LDS(p) ((__attribute__((address_space(3))) void *)(p))
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+static constexpr int kSpanTile = 32;        // cache rows per tile
+static constexpr float kSpanSlack = 8.f;    // how far (in powers of two) a weight may exceed the running reference
+
+__device__ __forceinline__ float span_ror8(float v) {  // lane l of a row of 16 receives lane (l + 8) % 16
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float span_max_groups(float v) {  // over the four lane groups that hold one column
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    return fmaxf(v, __shfl_xor(v, 32, 64));
 }
 
-// One wavefront per (sequence, token, query head): scores to the workspace, softmax, weighted sum.
-__global__ __launch_bounds__(64) void span_attention_kernel(SpanArgs a) {
-    const int u = blockIdx.x % a.Hq, t = blockIdx.x / a.Hq, b = blockIdx.y, lane = threadIdx.x, hd = a.hd;
-    if (a.d_span && t >= a.d_span[b]) return;
-    int n = a.d_len[b];
-    n = n < 0 ? 0 : (n > a.S ? a.S : n);
-    n = n + t + 1 < a.S ? n + t + 1 : a.S;
-    const int kvh = u / (a.Hq / a.Hkv);
-    const size_t m = (size_t)b * a.T + t;
-    const float *q = a.q + (m * a.Hq + u) * hd;
-    float *sc = a.ws + (m * a.Hq + u) * a.S;
-    const float scale = rsqrtf((float)hd);
-    float mx = -INFINITY;
-    for (int j = lane; j < n; j += 64) {
-        const size_t rowi = kv_row_index(a.map, b, kvh, a.Hkv, a.S, j);
-        float s = 0.f;
-        for (int e = 0; e < hd; ++e) s += q[e] * span_elem(a.kc + rowi * hd, e, a.map.kscale, rowi);
-        s *= scale;
-        sc[j] = s;
-        mx = fmaxf(mx, s);
-        if (s != s) mx = s;
-    }
-    mx = wave_max(mx);
-    float den = 0.f;
-    for (int j = lane; j < n; j += 64) { sc[j] = expf(sc[j] - mx); den += sc[j]; }
-    den = wave_sum(den);
-    __syncthreads();
-    for (int j = lane; j < n; j += 64) sc[j] /= den;
-    __syncthreads();
-    for (int e = lane; e < hd; e += 64) {
-        float o = 0.f;
-        for (int j = 0; j < n; ++j) {
-            const size_t rowi = kv_row_index(a.map, b, kvh, a.Hkv, a.S, j);
-            o += sc[j] * span_elem(a.vc + rowi * hd, e, a.map.vscale, rowi);
+// Rows of the workspace: statistics (max, sum) of every (query row, split), then partial outputs (nsplit > 1), then scores (weights).
+struct SpanWs {
+    size_t stats, part, scores, total;  // offsets in floats
+    int ld;                             // floats per row of scores
+};
+__host__ __device__ static inline SpanWs span_ws(int B, int T, int Hq, int hd, int S, int nsplit, bool weights) {
+    SpanWs w;
+    const size_t rows = (size_t)B * T * Hq;
+    w.ld = (S + kSpanTile - 1) / kSpanTile * kSpanTile;
+    w.stats = 0;
+    w.part = nsplit > 1 || weights ? (rows * nsplit * 2 + 3) / 4 * 4 : 0;
+    w.scores = w.part + (nsplit > 1 ? rows * nsplit * hd : 0);
+    w.total = w.scores + (weights ? rows * w.ld : 0);
+    return w;
+}
+
+// What a sequence's span looks like: rows that were there, new tokens.
+__device__ __forceinline__ void span_extent(const SpanArgs &a, int b, int *n0, int *tn) {
+    int n = a.d_len[b], t = a.T;
+    if (a.d_span) { const int s = a.d_span[b]; t = s < 0 ? 0 : (s < t ? s : t); }
+    *n0 = n < 0 ? 0 : (n > a.S ? a.S : n);
+    *tn = t;
+}
+
+// ONCE: no other workgroup reads these cache rows (one row tile), so their copies are non-temporal: they stream faster.
+template <int HD, int NT, int W, bool I16, bool ONCE>
+__global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int row_tiles, int items) {
+    constexpr int RB = HD * 2;                    // bytes of a cache row
+    constexpr int KS = HD / 32, OT = HD / 16;     // k-steps of a score, tiles of the output
+    constexpr int TILEB = kSpanTile * RB;
+    constexpr int STAGE = 2 * TILEB + (I16 ? 512 : 0);
+    constexpr int NST = HD == 128 ? 2 : 4;        // 32 KB of ring per wavefront: five of them, or one workgroup of four, per compute unit
+    constexpr int LPR = RB / 16;                  // lanes per row of a copy instruction
+    constexpr int ROWS = 8 * NT;                  // query rows of this workgroup
+    __shared__ __attribute__((aligned(1024))) unsigned char ring_all[W * NST * STAGE];
+    static_assert(ROWS * (HD + 2) * 4 <= NST * STAGE, "the join reuses the ring");
+
+    // Row tiles of one item run at the same time on the same XCD (workgroups that are congruent modulo 8 share one).
+    const int bid = blockIdx.x, rem = bid % (8 * row_tiles);
+    const int rt = rem / 8;
+    int item = bid / (8 * row_tiles) * 8 + rem % 8;
+    if (item >= items) return;
+    const int split = item % a.nsplit; item /= a.nsplit;
+    const int kvh = item % a.Hkv, b = item / a.Hkv;
+    const int G = a.Hq / a.Hkv;
+    int n0, tn;
+    span_extent(a, b, &n0, &tn);
+    n0 = __builtin_amdgcn_readfirstlane(n0);
+    tn = __builtin_amdgcn_readfirstlane(tn);
+    const int R = tn * G, r0 = rt * ROWS;
+    if (r0 >= R) return;
+    const int rlast = (R < r0 + ROWS ? R : r0 + ROWS) - 1;
+    auto limit = [&](int rr) { const int n = n0 + rr / G + 1; return n < a.S ? n : a.S; };  // rows that query row rr sees
+    const int nmax = limit(rlast), nmin = limit(r0);
+
+    const int wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int c = lane & 15, j = lane >> 4;       // column / group of 4 keys
+    unsigned char *ring = ring_all + wave * (NST * STAGE);
+    const int parts = a.nsplit * W;
+    const int chunk = ((nmax + parts - 1) / parts + kSpanTile - 1) / kSpanTile * kSpanTile;
+    const int64_t start = (int64_t)(split * W + wave) * chunk;
+    const int j0 = __builtin_amdgcn_readfirstlane(start < nmax ? (int)start : nmax);
+    const int j1 = __builtin_amdgcn_readfirstlane(nmax - j0 > chunk ? j0 + chunk : nmax);
+    const int ntiles = (j1 - j0 + kSpanTile - 1) / kSpanTile;
+
+    // ---- Q^T operands: column c of tile nt = query row r0 + 8 nt + (c & 7), term c >> 3; k-step s covers elements 32 s + 8 j + 0..7
+    f16x8_t qf[NT][KS];
+    int lim[NT];
+    const float qscale = rsqrtf((float)HD) * 1.44269504f;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int rr = r0 + 8 * nt + (c & 7);
+        const bool ok = rr <= rlast;
+        const int rc = ok ? rr : rlast;
+        lim[nt] = limit(rc);
+        const float *qp = a.q + (((size_t)b * a.T + rc / G) * a.Hq + kvh * G + rc % G) * HD + 8 * j;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const f32x4_t x0 = *reinterpret_cast<const f32x4_t *>(qp + 32 * s), x1 = *reinterpret_cast<const f32x4_t *>(qp + 32 * s + 4);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = ok ? (e < 4 ? x0[e & 3] : x1[e & 3]) * qscale : 0.f;
+                const _Float16 hi = (_Float16)__builtin_amdgcn_fmed3f(v, -65504.f, 65504.f);  // saturating, like every half here
+                const _Float16 lo = (_Float16)__builtin_amdgcn_fmed3f(v - (float)hi, -65504.f, 65504.f);
+                qf[nt][s][e] = c < 8 ? hi : lo;
+            }
         }
-        const f16_t h = f32_to_f16(o);
-        a.out[(m * a.Hq + u) * hd + e] = h;
-        if (a.out_lo) a.out_lo[(m * a.Hq + u) * hd + e] = f32_to_f16(o - f16_to_f32(h));
+    }
+
+    // ---- copies: instruction i of 16 rows moves rows (64 / LPR) i ..; this lane fills slot lane % LPR of row (64 / LPR) i + lane / LPR
+    constexpr int CI = 16 * RB / 1024;
+    auto kperm = [](int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; };
+    auto vperm = [](int r) { return HD == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); };
+    uint32_t ksrc[CI], vsrc[CI];
+#pragma unroll
+    for (int i = 0; i < CI; ++i) {
+        const int r = (64 / LPR) * i + lane / LPR, slot = lane % LPR;
+        ksrc[i] = (uint32_t)(r * RB + ((slot ^ kperm(r)) << 4));
+        vsrc[i] = (uint32_t)(r * RB + ((slot ^ vperm(r)) << 4));
+    }
+    // Page numbers: 64 entries of the sequence's list in a register, one per lane (a load per tile would wait for the copies
+    // in flight, which return in order).
+    const int32_t *pages = a.map.table ? a.map.table + (size_t)b * a.map.table_stride : nullptr;
+    const int last_page = pages && ntiles ? (j1 - 1) >> a.map.page_shift : 0;
+    int page_base = 0, page_reg = 0;
+    auto load_pages = [&](int from) {
+        page_base = from;
+        const int at = from + lane < last_page ? from + lane : last_page;
+        page_reg = pages[at];
+        asm volatile("" : "+v"(page_reg));        // waited for here, not at every use
+    };
+    if (pages && ntiles) load_pages(j0 >> a.map.page_shift);
+    const size_t slab = ((size_t)b * a.Hkv + kvh) * a.S;
+    auto row_of = [&](int row) -> size_t {        // row: the same in every lane, rows ascend from call to call
+        if (!pages) return slab + row;
+        const int at = row >> a.map.page_shift;
+        if (at - page_base >= 64) load_pages(at);
+        const int page = __builtin_amdgcn_readlane(page_reg, at - page_base);
+        return (((size_t)page * a.Hkv + kvh) << a.map.page_shift) + (row & ((1 << a.map.page_shift) - 1));
+    };
+    auto issue_tile = [&](int tile, int stage) {
+        if (tile >= ntiles) return;
+        unsigned char *st = ring + stage * STAGE;
+        size_t first[2];
+        int rows[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int row0 = j0 + tile * kSpanTile + 16 * h;
+            rows[h] = j1 - row0;                  // at most 16 of them exist; without any every lane is out of range
+            rows[h] = __builtin_amdgcn_readfirstlane(rows[h] < 0 ? 0 : (rows[h] > 16 ? 16 : rows[h]));
+            first[h] = rows[h] ? row_of(row0) : first[0];
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)first[h]), hi = __builtin_amdgcn_readfirstlane((uint32_t)(first[h] >> 32));
+            const size_t at = ((size_t)hi << 32 | lo) * HD;
+            __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<f16_t *>(a.kc + at), 0, rows[h] * RB, 0x00020000);
+            __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<f16_t *>(a.vc + at), 0, rows[h] * RB, 0x00020000);
+#pragma unroll
+            for (int i = 0; i < CI; ++i) {
+                unsigned char *kd = st + h * 16 * RB + i * 1024, *vd = kd + TILEB;
+#if defined(__HIP_DEVICE_COMPILE__)  // the host pass does not know this builtin
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, SPAN_LDS(kd), 16, (int)ksrc[i], 0, 0, ONCE ? 3 : 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, SPAN_LDS(vd), 16, (int)vsrc[i], 0, 0, ONCE ? 3 : 0);
+#else
+                (void)kd; (void)vd; (void)kr; (void)vr;
+#endif
+            }
+        }
+        if (I16) {  // row scales: lane l takes row l % 32 (the tile's first row where there is none: its weight is 0)
+            const int r = lane & 15, h = (lane >> 4) & 1;
+            const size_t at = h ? (r < rows[1] ? first[1] + r : first[0]) : (r < rows[0] ? first[0] + r : first[0]);
+#if defined(__HIP_DEVICE_COMPILE__)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a.map.kscale + at), SPAN_LDS(st + 2 * TILEB), 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a.map.vscale + at), SPAN_LDS(st + 2 * TILEB + 256), 4, 0, 0);
+#else
+            (void)at;
+#endif
+        }
+    };
+
+    int kaddr[KS], vaddr[OT];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) kaddr[s] = c * RB + (((4 * s + j) ^ kperm(c)) << 4);
+    {
+        const int r = 4 * j + (c >> 2);  // the row whose 4 elements this lane hands to the transposing read
+#pragma unroll
+        for (int t = 0; t < OT; ++t) vaddr[t] = TILEB + r * RB + (((2 * t + ((c >> 1) & 1)) ^ vperm(r)) << 4) + 8 * (c & 1);
+    }
+
+    f32x4_t acc[NT][OT];
+    float mrun[NT], den[NT], ref[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        mrun[nt] = -INFINITY; den[nt] = 0.f; ref[nt] = 0.f;
+#pragma unroll
+        for (int t = 0; t < OT; ++t) acc[nt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    const SpanWs w = span_ws(a.B, a.T, a.Hq, HD, a.S, a.nsplit, a.weight != nullptr);
+    const size_t row_base = ((size_t)b * a.Hkv + kvh) * a.T * G;  // query rows in the workspace: [b][kv head][t * G + g]
+    float *scores = a.ws + w.scores + row_base * w.ld;
+
+    auto consume = [&](int tile, unsigned char *st) {
+        const int key0 = j0 + tile * kSpanTile;
+        f32x4_t sacc[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sacc[nt][0] = sacc[nt][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const u32x4_t kw = *reinterpret_cast<const u32x4_t *>(st + h * 16 * RB + kaddr[s]);
+                if (I16) {
+                    const u32x4_t wh = {kw.x & 0xFFE0FFE0u, kw.y & 0xFFE0FFE0u, kw.z & 0xFFE0FFE0u, kw.w & 0xFFE0FFE0u};
+                    const u32x4_t wl = {kw.x & 0x001F001Fu, kw.y & 0x001F001Fu, kw.z & 0x001F001Fu, kw.w & 0x001F001Fu};
+                    const f16x8_t kh = __builtin_convertvector(__builtin_bit_cast(s16x8_t, wh), f16x8_t);
+                    const f16x8_t kl = __builtin_convertvector(__builtin_bit_cast(s16x8_t, wl), f16x8_t);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        sacc[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qf[nt][s], sacc[nt][h], 0, 0, 0);
+                        sacc[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, qf[nt][s], sacc[nt][h], 0, 0, 0);
+                    }
+                } else {
+                    const f16x8_t kf = __builtin_bit_cast(f16x8_t, kw);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) sacc[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[nt][s], sacc[nt][h], 0, 0, 0);
+                }
+            }
+        f32x4_t ksc[2], vsc[2];
+        if (I16) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                ksc[h] = *reinterpret_cast<const f32x4_t *>(st + 2 * TILEB + 64 * h + 16 * j);
+                vsc[h] = *reinterpret_cast<const f32x4_t *>(st + 2 * TILEB + 256 + 64 * h + 16 * j);
+            }
+        }
+        const bool tail = key0 + kSpanTile > nmin || key0 + kSpanTile > j1;  // some query row does not see all of these keys
+        if (!I16 && tail) {
+            // A value that is not finite must not reach the query rows that do not see its row (0 * inf is NaN): such elements are
+            // added to the others by hand and cleared from the tile.
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < TILEB / 1024; ++i) {
+                const u32x4_t x = *reinterpret_cast<const u32x4_t *>(st + TILEB + i * 1024 + lane * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7c00u) == 0x7c00u || (x[e] & 0x7c000000u) == 0x7c000000u;
+            }
+            if (__any(bad)) {
+                for (int k = 0; k < kSpanTile; ++k)
+#pragma unroll
+                    for (int t = 0; t < OT; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int e = 16 * t + 4 * j + i, kr = k & 15;
+                            f16_t *p = reinterpret_cast<f16_t *>(st + TILEB + k * RB + (((e >> 3) ^ vperm(kr)) << 4) + (e & 7) * 2);
+                            const f16_t v = *p;
+                            if ((v & 0x7c00u) == 0x7c00u) {
+#pragma unroll
+                                for (int nt = 0; nt < NT; ++nt)
+                                    if (c < 8 && key0 + k < lim[nt]) acc[nt][t][i] += f16_to_f32(v);
+                            }
+                        }
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int i = 0; i < TILEB / 1024; ++i) {
+                    u32x4_t *p = reinterpret_cast<u32x4_t *>(st + TILEB + i * 1024 + lane * 16);
+                    u32x4_t x = *p;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if ((x[e] & 0x7c00u) == 0x7c00u) x[e] &= 0xffff0000u;
+                        if ((x[e] & 0x7c000000u) == 0x7c000000u) x[e] &= 0xffffu;
+                    }
+                    *p = x;
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+        f16x8_t pf[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float x = sacc[nt][e >> 2][e & 3];
+                x += span_ror8(x);                // high and low term of the query row
+                if (I16) x *= ksc[e >> 2][e & 3];
+                v[e] = x;
+            }
+            if (tail) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (key0 + 16 * (e >> 2) + 4 * j + (e & 3) >= (lim[nt] < j1 ? lim[nt] : j1)) v[e] = -INFINITY;
+            }
+            if (a.weight && c < 8 && r0 + 8 * nt + c <= rlast) {
+                float *sp = scores + (size_t)(r0 + 8 * nt + c) * w.ld + key0 + 4 * j;
+                *reinterpret_cast<f32x4_t *>(sp) = f32x4_t{v[0], v[1], v[2], v[3]};
+                *reinterpret_cast<f32x4_t *>(sp + 16) = f32x4_t{v[4], v[5], v[6], v[7]};
+            }
+            float tmax = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+            if (__any(tmax > mrun[nt] + kSpanSlack)) {
+                const float mnew = fmaxf(mrun[nt], span_max_groups(tmax));
+                const float alpha = mrun[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mrun[nt] - mnew);
+                mrun[nt] = mnew;
+                den[nt] *= alpha;
+#pragma unroll
+                for (int t = 0; t < OT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[nt][t][i] *= alpha;
+            }
+            const float m = mrun[nt] == -INFINITY ? 0.f : mrun[nt];  // nothing seen yet: all weights are 0
+            float wmax = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] = __builtin_amdgcn_exp2f(v[e] - m);
+                den[nt] += v[e];
+            }
+            float inv = 1.f;
+            if (I16) {
+                // The row scale of V rides on the probability.  Scales are far below the normal range of a half, so the weights are
+                // measured in a reference per query row that follows their largest.
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int key = key0 + 16 * (e >> 2) + 4 * j + (e & 3);
+                    v[e] = tail && key >= (lim[nt] < j1 ? lim[nt] : j1) ? 0.f : v[e] * vsc[e >> 2][e & 3];
+                    wmax = fmaxf(wmax, v[e]);
+                }
+                if (__any(wmax > ref[nt] * 256.f)) {
+                    const float rnew = fmaxf(ref[nt], span_max_groups(wmax));
+                    const float beta = rnew > 0.f ? ref[nt] / rnew : 0.f;
+                    ref[nt] = rnew;
+#pragma unroll
+                    for (int t = 0; t < OT; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[nt][t][i] *= beta;
+                }
+                inv = ref[nt] > 0.f ? __builtin_amdgcn_rcpf(ref[nt]) : 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = I16 ? v[e] * inv : v[e];
+                const _Float16 hi = (_Float16)x;
+                pf[nt][e] = c < 8 ? hi : (_Float16)(x - (float)hi);
+            }
+        }
+        s16x4_t vt[OT][2];
+#if defined(__HIP_DEVICE_COMPILE__)
+        {
+            // Transposing reads: lane group j of 16 lanes receives the 4 keys of its group, one element per lane.  In assembly because the
+            // compiler takes the builtin for a reader of every copy in flight and waits for them.
+            const uint32_t sa = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)st;
+#pragma unroll
+            for (int t = 0; t < OT; t += 4)
+                asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+                             "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+                             "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+                             "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\ts_waitcnt lgkmcnt(0)"
+                             : "=&v"(vt[t][0]), "=&v"(vt[t][1]), "=&v"(vt[t + 1][0]), "=&v"(vt[t + 1][1]), "=&v"(vt[t + 2][0]), "=&v"(vt[t + 2][1]),
+                               "=&v"(vt[t + 3][0]), "=&v"(vt[t + 3][1])
+                             : "v"(sa + vaddr[t]), "v"(sa + vaddr[t + 1]), "v"(sa + vaddr[t + 2]), "v"(sa + vaddr[t + 3]), "n"(16 * RB)
+                             : "memory");
+        }
+#endif
+#pragma unroll
+        for (int t = 0; t < OT; ++t) {
+            const s16x8_t vw = __builtin_shufflevector(vt[t][0], vt[t][1], 0, 1, 2, 3, 4, 5, 6, 7);
+            if (I16) {
+                const f16x8_t vh = __builtin_convertvector(vw & (short)0xFFE0, f16x8_t), vl = __builtin_convertvector(vw & (short)0x001F, f16x8_t);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, pf[nt], acc[nt][t], 0, 0, 0);
+                    acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, pf[nt], acc[nt][t], 0, 0, 0);
+                }
+            } else {
+                const f16x8_t vf = __builtin_bit_cast(f16x8_t, vw);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[nt], acc[nt][t], 0, 0, 0);
+            }
+        }
+    };
+
+#pragma unroll
+    for (int k = 0; k < NST - 1; ++k) issue_tile(k, k);
+    __builtin_amdgcn_sched_barrier(0);
+    // A tile has landed once at most the copies of NST - 2 younger tiles are pending; the score stores between them count too, so
+    // with weights everything is waited for (as at the end, where fewer tiles are in flight).
+    constexpr int YOUNGER = (4 * CI + (I16 ? 2 : 0)) * (NST - 2);
+    static_assert(YOUNGER < 64, "vmcnt is a 6-bit counter");
+    for (int tile = 0, stage = 0; tile < ntiles; ++tile) {
+        if (YOUNGER > 0 && !a.weight && tile + NST - 2 < ntiles)
+            __builtin_amdgcn_s_waitcnt((YOUNGER & 15) | (7 << 4) | (15 << 8) | ((YOUNGER >> 4) << 14));  // vmcnt(YOUNGER) only
+        else
+            __builtin_amdgcn_s_waitcnt((0 & 15) | (7 << 4) | (15 << 8) | (0 << 14));                     // vmcnt(0)
+        __builtin_amdgcn_sched_barrier(0);
+        const int free_stage = stage == 0 ? NST - 1 : stage - 1;  // the stage consumed one step ago
+        issue_tile(tile + NST - 1, free_stage);
+        __builtin_amdgcn_sched_barrier(0);
+        consume(tile, ring + stage * STAGE);
+        __builtin_amdgcn_sched_barrier(0);
+        stage = stage == NST - 1 ? 0 : stage + 1;
+    }
+
+    // ---- join the wavefronts: the lane groups j hold disjoint keys (den), columns c and c + 8 the two terms of a query row (acc)
+    // over the wavefront's ring (all copies have landed): [ROWS][HD] sums, [ROWS] maxima, [ROWS] denominators
+    float *part = reinterpret_cast<float *>(ring);
+    auto s_max = [&](int i, int r) -> float & { return reinterpret_cast<float *>(ring_all + i * (NST * STAGE))[ROWS * HD + r]; };
+    auto s_den = [&](int i, int r) -> float & { return reinterpret_cast<float *>(ring_all + i * (NST * STAGE))[ROWS * (HD + 1) + r]; };
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        float d = den[nt];
+        d += __shfl_xor(d, 16, 64);
+        d += __shfl_xor(d, 32, 64);
+        if (j == 0 && c < 8) { s_max(wave, 8 * nt + c) = mrun[nt]; s_den(wave, 8 * nt + c) = d; }
+#pragma unroll
+        for (int t = 0; t < OT; ++t) {
+            f32x4_t o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = acc[nt][t][i] + span_ror8(acc[nt][t][i]);
+            if (I16) o = o * ref[nt];
+            if (c < 8) *reinterpret_cast<f32x4_t *>(part + (8 * nt + c) * HD + 16 * t + 4 * j) = o;
+        }
+    }
+    __syncthreads();
+    constexpr int TPR = HD / 8;                     // threads per query row, 8 elements each
+    for (int r = threadIdx.x / TPR; r < ROWS && r0 + r <= rlast; r += 64 * W / TPR) {
+        const int e0 = (threadIdx.x % TPR) * 8;
+        float m = s_max(0, r);
+#pragma unroll
+        for (int i = 1; i < W; ++i) m = fmaxf(m, s_max(i, r));
+        float d = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float f = s_max(i, r) == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_max(i, r) - m);
+            if (s_max(i, r) == -INFINITY && !(s_den(i, r) != s_den(i, r))) continue;  // a part without visible keys
+            d += s_den(i, r) * f;
+            const float *p = reinterpret_cast<const float *>(ring_all + i * (NST * STAGE)) + r * HD + e0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] += p[e] * f;
+        }
+        const int rr = r0 + r;
+        const size_t row = row_base + rr;
+        if (a.nsplit > 1 || a.weight) {
+            if (e0 == 0) {
+                a.ws[w.stats + (row * a.nsplit + split) * 2] = m;
+                a.ws[w.stats + (row * a.nsplit + split) * 2 + 1] = d;
+            }
+        }
+        if (a.nsplit > 1) {
+            float *p = a.ws + w.part + (row * a.nsplit + split) * HD + e0;
+            *reinterpret_cast<f32x4_t *>(p) = f32x4_t{o[0], o[1], o[2], o[3]};
+            *reinterpret_cast<f32x4_t *>(p + 4) = f32x4_t{o[4], o[5], o[6], o[7]};
+        } else {
+            const float inv = 1.0f / d;
+            const size_t at = (((size_t)b * a.T + rr / G) * a.Hq + kvh * G + rr % G) * HD + e0;
+            u32x4_t h, l;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                h[e] = pack_f16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
+                l[e] = pack_f16x2_lo(o[2 * e] * inv, o[2 * e + 1] * inv, h[e]);
+            }
+            *reinterpret_cast<u32x4_t *>(a.out + at) = h;
+            if (a.out_lo) *reinterpret_cast<u32x4_t *>(a.out_lo + at) = l;
+        }
     }
 }
 
-// One thread per cached row: the probabilities of all queries that see it, token after token.
-__global__ __launch_bounds__(256) void span_weight_kernel(SpanArgs a) {
-    const int j = blockIdx.x * 256 + threadIdx.x, kvh = blockIdx.y, b = blockIdx.z, g = a.Hq / a.Hkv;
-    int n0 = a.d_len[b];
-    n0 = n0 < 0 ? 0 : (n0 > a.S ? a.S : n0);
-    int T = a.T;
-    if (a.d_span) T = a.d_span[b] < T ? a.d_span[b] : T;
-    if (j >= a.S || j >= n0 + T || T <= 0) return;
-    float w = 0.f;
-    for (int t = j < n0 ? 0 : j - n0; t < T; ++t)
-        for (int u = kvh * g; u < (kvh + 1) * g; ++u) w += a.ws[(((size_t)b * a.T + t) * a.Hq + u) * a.S + j];
-    a.weight[((size_t)b * a.Hkv + kvh) * a.S + j] += w;
+// Second launch: the first `merge_blocks` workgroups join the splits of 4 query rows each (a wavefront per row), the others add up
+// the weights of 1024 cache rows of a (sequence, kv head) each: exp2(score - max) / sum over the query rows, in their order.
+__global__ __launch_bounds__(256) void span_join_kernel(SpanArgs a, int merge_blocks, int key_blocks) {
+    __shared__ float s_m[256], s_inv[256];
+    const SpanWs w = span_ws(a.B, a.T, a.Hq, a.hd, a.S, a.nsplit, a.weight != nullptr);
+    const int G = a.Hq / a.Hkv;
+    if ((int)blockIdx.x < merge_blocks) {
+        const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+        const int lane = threadIdx.x & 63;
+        if (row >= (size_t)a.B * a.T * a.Hq) return;
+        const int rr = (int)(row % ((size_t)a.T * G));
+        const int kvh = (int)(row / ((size_t)a.T * G) % a.Hkv), b = (int)(row / ((size_t)a.T * a.Hq));
+        int n0, tn;
+        span_extent(a, b, &n0, &tn);
+        if (rr >= tn * G) return;
+        const float *st = a.ws + w.stats + row * a.nsplit * 2;
+        float m = -INFINITY;
+        for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, st[2 * s]);
+        float d = 0.f, o0 = 0.f, o1 = 0.f;
+        const int per = a.hd / 64;
+        for (int s = 0; s < a.nsplit; ++s) {
+            if (st[2 * s] == -INFINITY && !(st[2 * s + 1] != st[2 * s + 1])) continue;
+            const float f = st[2 * s] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[2 * s] - m);
+            d += st[2 * s + 1] * f;
+            const float *p = a.ws + w.part + (row * a.nsplit + s) * a.hd + lane * per;
+            o0 += p[0] * f;
+            if (per == 2) o1 += p[1] * f;
+        }
+        const float inv = 1.0f / d;
+        const size_t at = (((size_t)b * a.T + rr / G) * a.Hq + kvh * G + rr % G) * a.hd + lane * per;
+        if (per == 2) {
+            const uint32_t h = pack_f16x2(o0 * inv, o1 * inv);
+            *reinterpret_cast<uint32_t *>(a.out + at) = h;
+            if (a.out_lo) *reinterpret_cast<uint32_t *>(a.out_lo + at) = pack_f16x2_lo(o0 * inv, o1 * inv, h);
+        } else {
+            const f16_t h = f32_to_f16(o0 * inv);
+            a.out[at] = h;
+            if (a.out_lo) a.out_lo[at] = f32_to_f16(o0 * inv - f16_to_f32(h));
+        }
+        return;
+    }
+    const int blk = blockIdx.x - merge_blocks;
+    const int slab = blk / key_blocks, key = (blk % key_blocks) * 1024 + threadIdx.x * 4;
+    const int b = slab / a.Hkv;
+    int n0, tn;
+    span_extent(a, b, &n0, &tn);
+    const int n = n0 + tn < a.S ? n0 + tn : a.S;  // rows that the last token sees
+    if (tn == 0 || (blk % key_blocks) * 1024 >= n) return;
+    const size_t row0 = (size_t)slab * a.T * G;
+    const float *sc = a.ws + w.scores + row0 * w.ld + key;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int rr0 = 0; rr0 < tn * G; rr0 += 256) {
+        __syncthreads();
+        const int mine = rr0 + threadIdx.x;
+        if (mine < tn * G) {
+            const float *st = a.ws + w.stats + (row0 + mine) * a.nsplit * 2;
+            float m = -INFINITY, d = 0.f;
+            for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, st[2 * s]);
+            for (int s = 0; s < a.nsplit; ++s)
+                if (st[2 * s] != -INFINITY || st[2 * s + 1] != st[2 * s + 1]) d += st[2 * s + 1] * __builtin_amdgcn_exp2f(st[2 * s] - m);
+            s_m[threadIdx.x] = m;
+            s_inv[threadIdx.x] = 1.0f / d;
+        }
+        __syncthreads();
+        const int count = tn * G - rr0 < 256 ? tn * G - rr0 : 256;
+        if (key < n)
+#pragma unroll 4
+            for (int r = 0; r < count; ++r) {
+                int lim = n0 + (rr0 + r) / G + 1;
+                lim = lim < a.S ? lim : a.S;
+                const f32x4_t s = *reinterpret_cast<const f32x4_t *>(sc + (size_t)(rr0 + r) * w.ld);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (key + i < lim) sum[i] += __builtin_amdgcn_exp2f(s[i] - s_m[r]) * s_inv[r];
+            }
+    }
+    float *wt = a.weight + (size_t)slab * a.S + key;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (key + i < n) wt[i] += sum[i];
 }
 
-int span_attention_splits(int B, int T, int Hq, int Hkv, int hd, int S) { return 1; }
+// Query rows of a workgroup: as many column tiles as the rows fill, up to four.
+static int span_tiles(int T, int G) {
+    const int R = T * G;
+    return R <= 8 ? 1 : R <= 16 ? 2 : 4;
+}
+static int64_t span_items(int B, int T, int Hq, int Hkv) {
+    const int G = Hq / Hkv, rows = 8 * span_tiles(T, G);
+    return (int64_t)B * Hkv * ((T * (int64_t)G + rows - 1) / rows);
+}
+
+int span_attention_splits(int B, int T, int Hq, int Hkv, int hd, int S) {
+    const int64_t items = span_items(B, T, Hq, Hkv);
+    int64_t s = items > 0 ? 256 / items : 1;         // one workgroup per compute unit
+    const int cap = S / 512;                          // each with 512 rows at least at full length
+    if (s > cap) s = cap;
+    if (s > 64) s = 64;
+    return s < 1 ? 1 : (int)s;
+}
 
 size_t span_attention_ws_floats(int B, int T, int Hq, int Hkv, int hd, int S, int nsplit, bool weights) {
-    return (size_t)B * T * Hq * S;
+    return span_ws(B, T, Hq, hd, S, nsplit, weights).total;
+}
+
+template <int HD, int NT, bool I16, bool ONCE>
+static void span_launch(const SpanArgs &a, int row_tiles, hipStream_t st) {
+    const int items = a.B * a.Hkv * a.nsplit;
+    const unsigned blocks = (unsigned)((int64_t)ceil_div(items, 8) * 8 * row_tiles);
+    // wavefronts that share a sequence's rows: enough of them for the compute units when there are few items
+    const int64_t work = (int64_t)items * row_tiles;
+    if (work <= 256) span_attention_kernel<HD, NT, 4, I16, ONCE><<<blocks, 256, 0, st>>>(a, row_tiles, items);
+    else if (work <= 512) span_attention_kernel<HD, NT, 2, I16, ONCE><<<blocks, 128, 0, st>>>(a, row_tiles, items);
+    else span_attention_kernel<HD, NT, 1, I16, ONCE><<<blocks, 64, 0, st>>>(a, row_tiles, items);
+}
+template <int HD, bool I16>
+static void span_launch_tiles(const SpanArgs &a, hipStream_t st) {
+    const int G = a.Hq / a.Hkv, nt = span_tiles(a.T, G);
+    const int row_tiles = (int)((a.T * (int64_t)G + 8 * nt - 1) / (8 * nt));
+    if (nt == 1) span_launch<HD, 1, I16, true>(a, 1, st);
+    else if (nt == 2) span_launch<HD, 2, I16, true>(a, 1, st);
+    else if (row_tiles == 1) span_launch<HD, 4, I16, true>(a, 1, st);
+    else span_launch<HD, 4, I16, false>(a, row_tiles, st);
 }
 
 void launch_span_attention(const SpanArgs &a, hipStream_t st) {
     if (a.B <= 0) return;
-    span_attention_kernel<<<dim3(a.T * a.Hq, a.B), 64, 0, st>>>(a);
-    if (a.weight) span_weight_kernel<<<dim3(ceil_div(a.S, 256), a.Hkv, a.B), 256, 0, st>>>(a);
+    if (a.hd == 128) a.map.kscale ? span_launch_tiles<128, true>(a, st) : span_launch_tiles<128, false>(a, st);
+    else a.map.kscale ? span_launch_tiles<64, true>(a, st) : span_launch_tiles<64, false>(a, st);
+    const int merge_blocks = a.nsplit > 1 ? (int)(((int64_t)a.B * a.T * a.Hq + 3) / 4) : 0;
+    const int key_blocks = a.weight ? ceil_div(a.S, 1024) : 0;
+    const int64_t blocks = merge_blocks + (int64_t)a.B * a.Hkv * key_blocks;
+    if (blocks > 0) span_join_kernel<<<(unsigned)blocks, 256, 0, st>>>(a, merge_blocks, key_blocks ? key_blocks : 1);
 }

@@ -1704,7 +1704,7 @@ int rl_op_logprob_gather(const float *logits, int64_t ld, int32_t M, int32_t V, 
 static int span_cache_map(const void *kc, const void *vc, const float *kscale, const float *vscale, const int32_t *table, int32_t table_stride,
                           int32_t page_size, int32_t B, int32_t Hkv, int32_t hd, int32_t S, KvMap *map) {
     if (!kc || !vc || (kscale == nullptr) != (vscale == nullptr)) return RL_GEN_E_NULL;
-    if (B < 0 || Hkv <= 0 || (hd != 64 && hd != 128) || S <= 0 || (int64_t)B * Hkv > INT32_MAX / 64) return RL_GEN_E_SHAPE;
+    if (B < 0 || Hkv <= 0 || (hd != 64 && hd != 128) || S <= 0 || S > 1 << 30 || (int64_t)B * Hkv > INT32_MAX / 64) return RL_GEN_E_SHAPE;
     if (((uintptr_t)kc | (uintptr_t)vc) % 16) return RL_GEN_E_SHAPE;
     map->kscale = const_cast<float *>(kscale); map->vscale = const_cast<float *>(vscale);
     if (table) {
