@@ -1,8 +1,18 @@
 // Verification of drafted tokens against the target's probabilities (rl_op_verify_drafts).
+//
+// With x a logits row, m its largest value and z = sum_v exp((x_v - m) / temperature), p_v = exp((x_v - m) / temperature) / z.  Every row
+// is read once (vd_rows_kernel: maximum, its index, sum, per chunk of the vocabulary); a sequence's first rejection then
+// follows from one probability pair per drafted token, and the next token from the weights max(0, p - q) or p of one row by inversion.
+//
+// A draw may land next to a border of the cumulative distribution, and a vocabulary of V tokens has V of them: weights with a
+// relative error e move a draw to a neighbour with a probability of the order of V * e, about one in a hundred for fp32 (1e-7) and
+// V = 128256.  So weights and sums are fp64: 2^g by rounding g to an integer with an addition, a polynomial of degree 8 (relative error
+// 1.1e-12 on [-1/2, 1/2]; interpolation at the Chebyshev nodes) and an addition to the exponent: 17 instructions per logit.  fp64
+// multiply-adds run at the rate of unpacked fp32 ones here, so the rows stay a stream from HBM.
 #include "kernels.h"
 
-#define VD_THREADS 1024
-#define VD_WAVES (VD_THREADS / RL_WAVE)
+#define VD_THREADS 256
+#define VD_PICK_THREADS 1024
 
 __device__ __forceinline__ double vd_wave_sum(double v) {
 #pragma unroll
@@ -10,151 +20,432 @@ __device__ __forceinline__ double vd_wave_sum(double v) {
     return v;
 }
 
-// A logits row: its largest value and lowest index (ties), whether it can be used, and the sum of exp((x - max) * inv).
-struct VdRow {
-    double max, sum;
-    int arg;
-    bool ok;
+// 2^g for -1020 <= g <= 1000.
+__device__ __forceinline__ double vd_exp2(double g) {
+    const double magic = 6755399441055744.0;  // 1.5 * 2^52: adding it leaves the nearest integer in the low bits
+    const double t = g + magic;
+    const double f = g - (t - magic);
+    double p = 1.3255224878668817e-06;
+    p = __builtin_fma(p, f, 1.5310079402249296e-05);
+    p = __builtin_fma(p, f, 0.00015403455852453838);
+    p = __builtin_fma(p, f, 0.0013333450568000645);
+    p = __builtin_fma(p, f, 0.009618129159402558);
+    p = __builtin_fma(p, f, 0.05550410941205933);
+    p = __builtin_fma(p, f, 0.2402265069581299);
+    p = __builtin_fma(p, f, 0.6931471805459335);
+    p = __builtin_fma(p, f, 1.0);
+    return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
+}
+// exp((x - m) / temperature) with c = log2(e) / temperature; 0 below 2^-1020 (and for x = -inf), which no sum notices.
+__device__ __forceinline__ double vd_weight(float x, double m, double c) {
+    const double g = ((double)x - m) * c;
+    const double w = vd_exp2(__builtin_fmax(g, -1020.0));
+    return g >= -1020.0 ? w : 0.0;
+}
+
+// Workspace: per (sequence, row, chunk) sum, maximum and index of the maximum (-1: the chunk holds a NaN); per sequence and target
+// row its maximum and sum; per (sequence, chunk) the weight of the decisive row; per sequence what was decided.
+struct VdDecision {
+    int stop, bad, rejected, token;  // first token not accepted; row unusable; draft rejected; the drafted token there
 };
-
-__device__ VdRow vd_row(const float *row, int V, double inv, bool greedy, double *redd, int *redi) {
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    float m = -INFINITY;
-    int arg = 0x7fffffff;
-    int nan = 0;
-    for (int i = tid; i < V; i += VD_THREADS) {
-        const float x = row[i];
-        nan |= x != x;
-        if (x > m || (x == m && i < arg)) { m = x; arg = i; }
+struct VdWs {
+    double *sum, *row_sum, *mass;
+    float *max, *row_max;
+    int32_t *arg;
+    VdDecision *dec;
+};
+__host__ __device__ static inline size_t vd_ws(void *base, int B, int T, int chunks, VdWs *w) {
+    const size_t rows = (size_t)B * (2 * T + 1), cells = rows * chunks, n8 = cells + rows + (size_t)B * chunks;
+    double *d = reinterpret_cast<double *>(base);
+    float *f = reinterpret_cast<float *>(d + n8);
+    if (w) {
+        w->sum = d; w->row_sum = d + cells; w->mass = d + cells + rows;
+        w->max = f; w->row_max = f + cells; w->arg = reinterpret_cast<int32_t *>(f + cells + rows);
+        w->dec = reinterpret_cast<VdDecision *>(f + 2 * cells + rows);
     }
-    for (int o = 32; o > 0; o >>= 1) {
-        const float om = __shfl_xor(m, o, 64);
-        const int oa = __shfl_xor(arg, o, 64);
-        nan |= __shfl_xor(nan, o, 64);
-        if (om > m || (om == m && oa < arg)) { m = om; arg = oa; }
-    }
-    __syncthreads();
-    if (lane == 0) { redd[wv] = m; redi[wv] = nan ? -1 : arg; }
-    __syncthreads();
-    VdRow r;
-    r.max = -INFINITY; r.arg = 0x7fffffff; r.ok = true; r.sum = 0;
-    for (int w = 0; w < VD_WAVES; ++w) {
-        if (redi[w] < 0) r.ok = false;
-        else if (redd[w] > r.max || (redd[w] == r.max && redi[w] < r.arg)) { r.max = redd[w]; r.arg = redi[w]; }
-    }
-    if (!greedy && !(fabs(r.max) < INFINITY)) r.ok = false;
-    __syncthreads();
-    double s = 0;
-    if (r.ok && fabs(r.max) < INFINITY)
-        for (int i = tid; i < V; i += VD_THREADS) s += exp(((double)row[i] - r.max) * inv);
-    s = vd_wave_sum(s);
-    if (lane == 0) redd[wv] = s;
-    __syncthreads();
-    for (int w = 0; w < VD_WAVES; ++w) r.sum += redd[w];
-    __syncthreads();
-    return r;
+    return n8 * 8 + (2 * cells + rows) * 4 + (size_t)B * sizeof(VdDecision);
 }
 
-// One workgroup per sequence, row after row.
-__global__ __launch_bounds__(VD_THREADS) void verify_drafts_kernel(VerifyArgs a) {
-    __shared__ double redd[VD_WAVES], s_pre;
-    __shared__ int redi[VD_WAVES], s_tok, s_owner;
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const bool greedy = !(a.temperature > 0);
-    const double inv = greedy ? 1.0 : 1.0 / a.temperature;
+__device__ __forceinline__ int vd_span(const VerifyArgs &a, int b) {
     int n = a.T;
-    if (a.d_span) n = a.d_span[b] < 0 ? 0 : (a.d_span[b] < n ? a.d_span[b] : n);
-    int32_t *tokens = a.tokens + (size_t)b * (a.T + 1);
-    float *logp = a.logp ? a.logp + (size_t)b * (a.T + 1) : nullptr;
-    int i = 0;
-    bool rejected = false, bad = false;
-    VdRow p, q;
-    const float *prow, *qrow = nullptr;
-    int x = -1;
-    for (;; ++i) {
-        prow = a.target + ((size_t)b * (a.T + 1) + i) * a.ldt;
-        p = vd_row(prow, a.V, inv, greedy, redd, redi);
-        bad = !p.ok;
-        if (bad || i == n) break;
-        x = a.drafts[(size_t)b * a.T + i];
-        const bool in = x >= 0 && x < a.V;
-        bool ok;
-        if (greedy) {
-            ok = x == p.arg;
-        } else {
-            double qx = 1.0;
-            if (a.draft) {
-                qrow = a.draft + ((size_t)b * a.T + i) * a.ldd;
-                q = vd_row(qrow, a.V, inv, false, redd, redi);
-                if (!q.ok) { bad = true; break; }
-                qx = in ? exp(((double)qrow[x] - q.max) * inv) / q.sum : 0.0;
+    if (a.d_span) { const int s = a.d_span[b]; n = s < 0 ? 0 : (s < n ? s : n); }
+    return n;
+}
+// Row r of a sequence: target rows 0 .. T, then draft rows.
+__device__ __forceinline__ const float *vd_row(const VerifyArgs &a, int b, int r) {
+    return r <= a.T ? a.target + ((size_t)b * (a.T + 1) + r) * a.ldt : a.draft + ((size_t)b * a.T + (r - a.T - 1)) * a.ldd;
+}
+
+// One workgroup per (row, chunk of 256 * EPT logits): the logits stay in registers between the maximum and the weights.  A wavefront's weights
+// refer to its own maximum (no barrier before them); the four wavefronts join at the end.  SUMS: off where only the largest is wanted.
+template <int EPT, bool SUMS>
+__global__ __launch_bounds__(VD_THREADS) void vd_rows_kernel(VerifyArgs a, int chunks, int rows) {
+    __shared__ double s_sum[4];
+    __shared__ float s_max[4];
+    __shared__ int s_arg[4];
+    const int chunk = blockIdx.x % chunks, cell_row = blockIdx.x / chunks, r = cell_row % rows, b = cell_row / rows;
+    const int n = vd_span(a, b);
+    if (r <= a.T ? r > n : r - a.T - 1 >= n) return;  // not reached in any case
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const float *row = vd_row(a, b, r);
+    const int first = chunk * (VD_THREADS * EPT);
+    const int left = a.V - first < VD_THREADS * EPT ? a.V - first : VD_THREADS * EPT;
+    row += first;
+    float x[EPT];
+    // element e of the thread: index 4 * (tid + 256 * (e / 4)) + e % 4, whole vectors where row and length allow them
+    if ((reinterpret_cast<uintptr_t>(row) & 15) == 0) {
+#pragma unroll
+        for (int k = 0; k < EPT / 4; ++k) {
+            const int i = 4 * (tid + VD_THREADS * k);
+            f32x4_t v = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            if (i + 4 <= left) {
+                v = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t *>(row + i));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i + e < left) v[e] = row[i + e];
             }
-            ok = in && (double)a.u[(size_t)b * (a.T + 1) + i] * qx < exp(((double)prow[x] - p.max) * inv) / p.sum;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[4 * k + e] = v[e];
         }
-        if (!ok) { rejected = true; break; }
-        if (tid == 0) {
-            tokens[i] = x;
-            if (logp) logp[i] = (float)(((double)prow[x] - p.max) * inv - log(p.sum));
-        }
-    }
-    int next = -1;
-    if (!bad && greedy) next = p.arg;
-    if (!bad && !greedy) {
-        auto weight = [&](int v, bool residual) -> double {
-            const double pv = exp(((double)prow[v] - p.max) * inv) / p.sum;
-            if (!residual) return pv;
-            const double qv = a.draft ? exp(((double)qrow[v] - q.max) * inv) / q.sum : (v == x ? 1.0 : 0.0);
-            return pv > qv ? pv - qv : 0.0;
-        };
-        const int seg = (a.V + VD_THREADS - 1) / VD_THREADS;
-        const int i0 = tid * seg < a.V ? tid * seg : a.V, i1 = i0 + seg < a.V ? i0 + seg : a.V;
-        for (int pass = 0; pass < 2; ++pass) {
-            const bool residual = rejected && pass == 0;
-            double s = 0;
-            for (int v = i0; v < i1; ++v) s += weight(v, residual);
-            double incl = s;
-            for (int o = 1; o < 64; o <<= 1) {
-                const double up = __shfl_up(incl, o, 64);
-                if (lane >= o) incl += up;
-            }
-            __syncthreads();
-            if (lane == 63) redd[wv] = incl;
-            if (tid == 0) { s_owner = VD_THREADS; s_tok = -1; s_pre = 0; }
-            __syncthreads();
-            double base = 0, total = 0;
-            for (int w = 0; w < VD_WAVES; ++w) { if (w < wv) base += redd[w]; total += redd[w]; }
-            if (residual && !(total > 0)) continue;
-            const double target = (double)a.u[(size_t)b * (a.T + 1) + a.T] * total;
-            if (s > 0 && base + incl > target) atomicMin(&s_owner, tid);
-            __syncthreads();
-            if (s_owner == VD_THREADS && s > 0) atomicMax(&s_tok, i1 - 1);  // rounding: the last segment with weight
-            if (tid == s_owner) {
-                double run = base + incl - s;
-                int last = i0;
-                for (int v = i0; v < i1; ++v) {
-                    const double w = weight(v, residual);
-                    if (w > 0) last = v;
-                    run += w;
-                    if (w > 0 && run > target) break;
-                }
-                s_tok = last;
-            }
-            __syncthreads();
-            next = s_tok;
-            break;
+    } else {
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) {
+            const int i = 4 * (tid + VD_THREADS * (e / 4)) + e % 4;
+            x[e] = i < left ? row[i] : -INFINITY;
         }
     }
+    float m = -INFINITY;
+    bool nan = false;
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) { nan |= x[e] != x[e]; m = fmaxf(m, x[e]); }
+    m = wave_max(m);
+    int arg = 0x7fffffff;
+#pragma unroll
+    for (int e = EPT - 1; e >= 0; --e)
+        if (x[e] == m) arg = 4 * (tid + VD_THREADS * (e / 4)) + e % 4;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const int other = __shfl_xor(arg, o, 64);
+        arg = other < arg ? other : arg;
+    }
+    double s = 0.0;
+    if (SUMS) {
+        const double md = m == -INFINITY ? 0.0 : (double)m, c = 1.4426950408889634074 / (a.temperature > 0 ? a.temperature : 1.0);
+        double s1 = 0.0;
+#pragma unroll
+        for (int e = 0; e < EPT; e += 2) {
+            s += vd_exp2(__builtin_fmax(((double)x[e] - md) * c, -1020.0));
+            s1 += vd_exp2(__builtin_fmax(((double)x[e + 1] - md) * c, -1020.0));
+        }
+        s = vd_wave_sum(s + s1);
+    }
+    nan = __any(nan);
+    if (lane == 0) { s_max[wv] = m; s_arg[wv] = nan ? -1 : arg; s_sum[wv] = s; }
+    __syncthreads();
     if (tid == 0) {
-        a.accepted[b] = i;
-        tokens[i] = next;
-        if (logp) logp[i] = next >= 0 ? (float)(((double)prow[next] - p.max) * inv - log(p.sum)) : 0.f;
-        for (int k = i + 1; k <= a.T; ++k) { tokens[k] = -1; if (logp) logp[k] = 0.f; }
+        const double c = 1.4426950408889634074 / (a.temperature > 0 ? a.temperature : 1.0);
+        float mm = s_max[0];
+        bool bad = s_arg[0] < 0;
+        int at = s_arg[0];
+        for (int w = 1; w < 4; ++w) {
+            bad |= s_arg[w] < 0;
+            if (s_max[w] > mm || (s_max[w] == mm && s_arg[w] < at)) { mm = s_max[w]; at = s_arg[w]; }
+        }
+        double total = 0.0;
+        if (SUMS)
+            for (int w = 0; w < 4; ++w)
+                if (s_max[w] != -INFINITY) total += s_sum[w] * vd_weight(s_max[w], mm, c);
+        VdWs w;
+        vd_ws(a.ws, a.B, a.T, chunks, &w);
+        const size_t cell = ((size_t)b * (2 * a.T + 1) + r) * chunks + chunk;
+        w.max[cell] = mm;
+        w.arg[cell] = bad ? -1 : (at < left ? at + first : 0x7fffffff);
+        w.sum[cell] = total;
     }
 }
 
-size_t verify_drafts_ws_bytes(int B, int T, int V) { return 256; }
+// What happens to sequence b, worked out by a whole workgroup (every thread returns it): rows joined from their chunks by a thread
+// each, then the first draft that is not accepted.  s_*: shared arrays of 2 T + 1 (T + 1 for s_arg) elements.
+template <int THREADS>
+__device__ VdDecision vd_decide(const VerifyArgs &a, const VdWs &w, int b, int chunks, bool sums, double *s_z, float *s_m, int *s_arg, int *s_stop) {
+    const int n = vd_span(a, b), T = a.T, tid = threadIdx.x;
+    const bool greedy = !(a.temperature > 0);
+    const double c = 1.4426950408889634074 / (greedy ? 1.0 : a.temperature);
+    const int rows = a.draft ? 2 * T + 1 : T + 1;
+    if (tid == 0) *s_stop = n;
+    for (int r = tid; r < rows; r += THREADS) {
+        if (r <= T ? r > n : r - T - 1 >= n) continue;
+        const size_t cell = ((size_t)b * (2 * T + 1) + r) * chunks;
+        float m = -INFINITY;
+        int arg = 0x7fffffff;
+        bool bad = false;
+        for (int k = 0; k < chunks; ++k) {
+            const float cm = w.max[cell + k];
+            const int ca = w.arg[cell + k];
+            bad |= ca < 0;
+            if (cm > m || (cm == m && ca < arg)) { m = cm; arg = ca; }
+        }
+        if (!greedy && !(fabsf(m) < INFINITY)) bad = true;
+        double z = 0.0;
+        if (sums && !bad && fabsf(m) < INFINITY)
+            for (int k = 0; k < chunks; ++k) {
+                const float cm = w.max[cell + k];
+                if (cm != -INFINITY) z += w.sum[cell + k] * vd_weight(cm, m, c);
+            }
+        s_m[r] = m;
+        s_z[r] = z;
+        s_arg[r] = bad ? -1 : arg;
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += THREADS) {
+        bool go = s_arg[i] >= 0;
+        const int x = a.drafts[(size_t)b * T + i];
+        if (greedy) {
+            go = go && x == s_arg[i];
+        } else if (go) {
+            const bool in = x >= 0 && x < a.V;
+            double q = 1.0;
+            if (a.draft) {
+                const int r = T + 1 + i;
+                go = s_arg[r] >= 0;
+                if (go && in) q = vd_weight(vd_row(a, b, r)[x], s_m[r], c) / s_z[r];
+            }
+            go = go && in && (double)a.u[(size_t)b * (T + 1) + i] * q < vd_weight(vd_row(a, b, i)[x], s_m[i], c) / s_z[i];
+        }
+        if (!go) atomicMin(s_stop, i);
+    }
+    __syncthreads();
+    VdDecision d;
+    d.stop = *s_stop;
+    d.bad = s_arg[d.stop] < 0 || (d.stop < n && a.draft && s_arg[T + 1 + d.stop] < 0);
+    d.rejected = d.stop < n;
+    d.token = d.rejected ? a.drafts[(size_t)b * T + d.stop] : -1;
+    return d;
+}
+
+#define VD_MAX_ROWS (2 * 256 + 1)
+
+// Weights max(0, p - q) of the rejected position, summed per chunk: one workgroup per (sequence, chunk).  The decision is worked out in
+// each (a launch of its own would cost more); the first chunk's workgroup keeps it for the choice.
+__global__ __launch_bounds__(VD_THREADS) void vd_residual_kernel(VerifyArgs a, int chunks, int chunk_len) {
+    __shared__ double s_z[VD_MAX_ROWS], s_sum[4];
+    __shared__ float s_m[VD_MAX_ROWS];
+    __shared__ int s_arg[VD_MAX_ROWS], s_stop;
+    const int chunk = blockIdx.x % chunks, b = blockIdx.x / chunks, tid = threadIdx.x;
+    VdWs w;
+    vd_ws(a.ws, a.B, a.T, chunks, &w);
+    const VdDecision d = vd_decide<VD_THREADS>(a, w, b, chunks, true, s_z, s_m, s_arg, &s_stop);
+    if (chunk == 0) {
+        if (tid == 0) w.dec[b] = d;
+        const int rows = 2 * a.T + 1;
+        for (int r = tid; r < rows; r += VD_THREADS)
+            if (r <= a.T ? r <= d.stop : r - a.T - 1 <= d.stop && d.rejected) {
+                w.row_max[(size_t)b * rows + r] = s_m[r];
+                w.row_sum[(size_t)b * rows + r] = s_z[r];
+            }
+    }
+    if (d.bad || !d.rejected) return;
+    const int rp = d.stop, rq = a.T + 1 + d.stop;
+    const double c = 1.4426950408889634074 / a.temperature, mp = s_m[rp], mq = s_m[rq], ip = 1.0 / s_z[rp], iq = 1.0 / s_z[rq];
+    const float *prow = vd_row(a, b, rp), *qrow = vd_row(a, b, rq);
+    const int first = chunk * chunk_len, last = first + chunk_len < a.V ? first + chunk_len : a.V;
+    double s = 0.0;
+#pragma unroll 4
+    for (int v = first + tid; v < last; v += VD_THREADS) {
+        const double e = vd_weight(prow[v], mp, c) * ip - vd_weight(qrow[v], mq, c) * iq;
+        s += e > 0.0 ? e : 0.0;
+    }
+    s = vd_wave_sum(s);
+    if ((tid & 63) == 0) s_sum[tid >> 6] = s;
+    __syncthreads();
+    if (tid == 0) w.mass[(size_t)b * chunks + chunk] = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
+}
+
+// The next token and the outputs: one workgroup per sequence.  DECIDE: no residual kernel ran (greedy, or drafts that were not
+// sampled), so the decision is worked out here.
+template <bool DECIDE>
+__global__ __launch_bounds__(VD_PICK_THREADS) void vd_pick_kernel(VerifyArgs a, int chunks, int chunk_len) {
+    constexpr int WAVES = VD_PICK_THREADS / RL_WAVE;
+    __shared__ double s_z[VD_MAX_ROWS], s_red[WAVES], s_before, s_total, s_part;
+    __shared__ float s_m[VD_MAX_ROWS];
+    __shared__ int s_arg[VD_MAX_ROWS], s_stop, s_chunk, s_owner, s_next;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, T = a.T, rows = 2 * T + 1;
+    const bool greedy = !(a.temperature > 0), sums = !greedy || a.logp;
+    const double c = 1.4426950408889634074 / (greedy ? 1.0 : a.temperature);
+    VdWs w;
+    vd_ws(a.ws, a.B, T, chunks, &w);
+    VdDecision d;
+    if (DECIDE) {
+        d = vd_decide<VD_PICK_THREADS>(a, w, b, chunks, sums, s_z, s_m, s_arg, &s_stop);
+    } else {
+        d = w.dec[b];
+        for (int r = tid; r < rows; r += VD_PICK_THREADS)
+            if (r <= T ? r <= d.stop : r - T - 1 == d.stop && d.rejected) {
+                s_m[r] = w.row_max[(size_t)b * rows + r];
+                s_z[r] = w.row_sum[(size_t)b * rows + r];
+            }
+        __syncthreads();
+    }
+    const float *prow = vd_row(a, b, d.stop);
+    int next = -1;
+    if (!d.bad && greedy) {
+        next = s_arg[d.stop];
+    } else if (!d.bad) {
+        const double mp = s_m[d.stop], ip = 1.0 / s_z[d.stop];
+        const bool sampled = d.rejected && a.draft;
+        const int rq = T + 1 + d.stop;
+        const float *qrow = sampled ? vd_row(a, b, rq) : nullptr;
+        const double mq = sampled ? (double)s_m[rq] : 0.0, iq = sampled ? 1.0 / s_z[rq] : 0.0;
+        bool residual = d.rejected;
+        auto weight = [&](int v) -> double {
+            const double p = vd_weight(prow[v], mp, c) * ip;
+            if (!residual) return p;
+            if (!sampled) return v == d.token ? 0.0 : p;
+            const double e = p - vd_weight(qrow[v], mq, c) * iq;
+            return e > 0.0 ? e : 0.0;
+        };
+        // a drafted token that was not sampled leaves its own chunk without its weight: that chunk is summed again
+        const int own = residual && !sampled && d.token >= 0 && d.token < a.V ? d.token / chunk_len : -1;
+        if (own >= 0) {
+            const int last = (own + 1) * chunk_len < a.V ? (own + 1) * chunk_len : a.V;
+            double s = 0.0;
+            for (int v = own * chunk_len + tid; v < last; v += VD_PICK_THREADS) s += weight(v);
+            s = vd_wave_sum(s);
+            if (lane == 0) s_red[wv] = s;
+            __syncthreads();
+            if (tid == 0) {
+                double t = 0.0;
+                for (int k = 0; k < WAVES; ++k) t += s_red[k];
+                s_part = t;
+            }
+            __syncthreads();
+        }
+        const size_t cell = ((size_t)b * rows + d.stop) * chunks;
+        auto mass = [&](int k) -> double {
+            if (residual && sampled) return w.mass[(size_t)b * chunks + k];
+            if (residual && k == own) return s_part;
+            const float cm = w.max[cell + k];
+            return cm == -INFINITY ? 0.0 : w.sum[cell + k] * vd_weight(cm, mp, c) * ip;
+        };
+        // the chunk that the draw falls into: the first whose running sum exceeds it (the last with weight, should none by rounding)
+        for (;;) {
+            if (wv == 0) {
+                double total = 0.0;
+                for (int k0 = 0; k0 < chunks; k0 += 64) {
+                    const double v = k0 + lane < chunks ? mass(k0 + lane) : 0.0;
+                    total += vd_wave_sum(v);
+                }
+                if (lane == 0) s_total = total;
+            }
+            __syncthreads();
+            if (!residual || s_total > 0.0) break;
+            residual = false;  // p and q are the same: p itself
+            __syncthreads();
+        }
+        const double target = (double)a.u[(size_t)b * (T + 1) + T] * s_total;
+        if (wv == 0) {
+            double before = 0.0, chosen_before = 0.0;
+            int chosen = -1, lastk = 0;
+            double last_before = 0.0;
+            for (int k0 = 0; k0 < chunks && chosen < 0; k0 += 64) {
+                const double v = k0 + lane < chunks ? mass(k0 + lane) : 0.0;
+                double incl = v;
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) {
+                    const double up = __shfl_up(incl, o, 64);
+                    if (lane >= o) incl += up;
+                }
+                const uint64_t over = __ballot(v > 0.0 && before + incl > target), some = __ballot(v > 0.0);
+                if (some) {
+                    const int l = 63 - __builtin_clzll(some);
+                    lastk = k0 + l;
+                    last_before = before + __shfl(incl - v, l, 64);
+                }
+                if (over) {
+                    const int l = __builtin_ctzll(over);
+                    chosen = k0 + l;
+                    chosen_before = before + __shfl(incl - v, l, 64);
+                }
+                before += __shfl(incl, 63, 64);
+            }
+            if (lane == 0) {
+                s_chunk = chosen >= 0 ? chosen : lastk;
+                s_before = chosen >= 0 ? chosen_before : last_before;
+                s_owner = VD_PICK_THREADS;
+                s_next = -1;
+            }
+        }
+        __syncthreads();
+        // within the chunk: every thread owns consecutive tokens, their sums are scanned in order, the first thread whose running sum
+        // exceeds the draw walks its own
+        const int first = s_chunk * chunk_len, last = first + chunk_len < a.V ? first + chunk_len : a.V;
+        const int per = (chunk_len + VD_PICK_THREADS - 1) / VD_PICK_THREADS;
+        const int i0 = first + tid * per < last ? first + tid * per : last, i1 = i0 + per < last ? i0 + per : last;
+        double s = 0.0;
+        for (int v = i0; v < i1; ++v) s += weight(v);
+        double incl = s;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const double up = __shfl_up(incl, o, 64);
+            if (lane >= o) incl += up;
+        }
+        if (lane == 63) s_red[wv] = incl;
+        __syncthreads();
+        double before = s_before;
+        for (int k = 0; k < wv; ++k) before += s_red[k];
+        if (s > 0.0 && before + incl > target) atomicMin(&s_owner, tid);
+        __syncthreads();
+        if (tid == s_owner) {
+            double run = before + incl - s;
+            int pick = i0;
+            for (int v = i0; v < i1; ++v) {
+                const double e = weight(v);
+                if (e > 0.0) pick = v;
+                run += e;
+                if (e > 0.0 && run > target) break;
+            }
+            s_next = pick;
+        } else if (s_owner == VD_PICK_THREADS && s > 0.0) {  // by rounding nobody's: the last token with weight
+            int pick = i0;
+            for (int v = i0; v < i1; ++v)
+                if (weight(v) > 0.0) pick = v;
+            atomicMax(&s_next, pick);
+        }
+        __syncthreads();
+        next = s_next;
+    }
+    int32_t *tokens = a.tokens + (size_t)b * (T + 1);
+    float *logp = a.logp ? a.logp + (size_t)b * (T + 1) : nullptr;
+    if (tid == 0) a.accepted[b] = d.stop;
+    for (int i = tid; i <= T; i += VD_PICK_THREADS) {
+        const int tok = i < d.stop ? a.drafts[(size_t)b * T + i] : (i == d.stop ? next : -1);
+        tokens[i] = tok;
+        if (logp) logp[i] = tok < 0 ? 0.f : (float)(((double)vd_row(a, b, i)[tok] - (double)s_m[i]) * (greedy ? 1.0 : 1.0 / a.temperature) - log(s_z[i]));
+    }
+}
+
+// Logits per workgroup: 8192 where that still gives every compute unit a few workgroups, else 2048.
+static int vd_per_thread(int B, int T, int V) { return (int64_t)B * (T + 1) * ceil_div(V, 8192) >= 512 ? 32 : 8; }
+
+size_t verify_drafts_ws_bytes(int B, int T, int V) {
+    return vd_ws(nullptr, B, T, ceil_div(V, VD_THREADS * vd_per_thread(B, T, V)), nullptr) + 8;
+}
 
 void launch_verify_drafts(const VerifyArgs &a, hipStream_t st) {
     if (a.B <= 0) return;
-    verify_drafts_kernel<<<a.B, VD_THREADS, 0, st>>>(a);
+    const int ept = vd_per_thread(a.B, a.T, a.V), chunk_len = VD_THREADS * ept, chunks = ceil_div(a.V, chunk_len);
+    const int rows = a.draft ? 2 * a.T + 1 : a.T + 1;
+    const unsigned blocks = (unsigned)((int64_t)a.B * rows * chunks);
+    const bool sums = a.temperature > 0 || a.logp;
+    if (ept == 32 && sums) vd_rows_kernel<32, true><<<blocks, VD_THREADS, 0, st>>>(a, chunks, rows);
+    else if (ept == 32) vd_rows_kernel<32, false><<<blocks, VD_THREADS, 0, st>>>(a, chunks, rows);
+    else if (sums) vd_rows_kernel<8, true><<<blocks, VD_THREADS, 0, st>>>(a, chunks, rows);
+    else vd_rows_kernel<8, false><<<blocks, VD_THREADS, 0, st>>>(a, chunks, rows);
+    if (a.draft) {
+        vd_residual_kernel<<<a.B * chunks, VD_THREADS, 0, st>>>(a, chunks, chunk_len);
+        vd_pick_kernel<false><<<a.B, VD_PICK_THREADS, 0, st>>>(a, chunks, chunk_len);
+    } else {
+        vd_pick_kernel<true><<<a.B, VD_PICK_THREADS, 0, st>>>(a, chunks, chunk_len);
+    }
 }
