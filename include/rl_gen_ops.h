@@ -264,14 +264,15 @@ int rl_op_rope_append_at(const float *qkv, int32_t nsplit, size_t split_stride, 
  * q fp32 [B*T, Hq*hd], rotated; out f16 [B*T, Hq*hd], out_lo its second half term or NULL.  T = 1 is decode attention.
  * weight (or NULL): weight[b, h, j] += the sum of p_j over the queries of kv head h and the span's valid tokens -- what
  * rl_op_evict_rows goes by.  Sums are formed in a fixed order (the same bits every time), also those of weight.
- * nsplit: workgroups that share the rows of a sequence, 1 .. 64, or 0: chosen from the shape.  ws fp32
- * [rl_op_span_attention_ws_floats(same arguments, weights = whether weight is given)] (may be NULL when that is 0), 16-byte aligned.
+ * nsplit: workgroups that share the rows of a sequence, 1 .. 64, or 0: chosen from the shape.  ws: fp32 workspace of ws_floats
+ * elements, 16-byte aligned, at least rl_op_span_attention_ws_floats(same arguments, weights = whether weight is given) of them (else
+ * RL_GEN_E_CAPACITY; may be NULL when that is 0).
  * A query sees a row whose K or V is not finite as a non-finite score or value; rows that a query does not see never reach
  * its result, whatever they hold.  Hq/Hkv <= 64. */
 int rl_op_span_attention(const float *q, const uint16_t *kc, const uint16_t *vc, const float *kscale, const float *vscale,
                          const int32_t *table, int32_t table_stride, int32_t page_size, const int32_t *d_len, const int32_t *d_span,
-                         uint16_t *out, uint16_t *out_lo, float *weight, float *ws, int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd,
-                         int32_t S, int32_t nsplit, void *hip_stream);
+                         uint16_t *out, uint16_t *out_lo, float *weight, float *ws, size_t ws_floats, int32_t B, int32_t T, int32_t Hq,
+                         int32_t Hkv, int32_t hd, int32_t S, int32_t nsplit, void *hip_stream);
 size_t rl_op_span_attention_ws_floats(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, int32_t S, int32_t nsplit,
                                       int32_t weights);
 
@@ -283,11 +284,11 @@ size_t rl_op_span_attention_ws_floats(int32_t B, int32_t T, int32_t Hq, int32_t 
  * above it (ascending): K and V rows and their scales, in place.  weight_out / pos_out: the values of the rows now in slots
  * 0 .. min(n, keep) - 1, entries behind are left as they were; each may be the array it is taken from (pos_out is required with pos).
  * d_len_out (DEVICE int32 [B], may be d_len, or NULL): min(n, keep).  1 <= keep <= S, 0 <= recent <= keep.
- * ws: DEVICE, rl_op_evict_rows_ws_bytes bytes, 8-byte aligned. */
+ * ws: DEVICE, ws_bytes long, 8-byte aligned, at least rl_op_evict_rows_ws_bytes (else RL_GEN_E_CAPACITY). */
 int rl_op_evict_rows(uint16_t *kc, uint16_t *vc, float *kscale, float *vscale, const int32_t *table, int32_t table_stride,
                      int32_t page_size, const float *weight, float *weight_out, const int32_t *pos, int32_t *pos_out, const int32_t *d_len,
-                     int32_t *d_len_out, void *ws, int32_t B, int32_t Hkv, int32_t hd, int32_t S, int32_t keep, int32_t recent,
-                     void *hip_stream);
+                     int32_t *d_len_out, void *ws, size_t ws_bytes, int32_t B, int32_t Hkv, int32_t hd, int32_t S, int32_t keep,
+                     int32_t recent, void *hip_stream);
 size_t rl_op_evict_rows_ws_bytes(int32_t B, int32_t Hkv, int32_t S, int32_t keep);
 
 /* Verification of drafted tokens with given random numbers, so that the tokens that come out are distributed as the target model's own.
@@ -305,10 +306,10 @@ size_t rl_op_evict_rows_ws_bytes(int32_t B, int32_t Hkv, int32_t S, int32_t keep
  * logp fp32 [B, T+1] or NULL: log p of each token of `tokens` under the target row it follows (temperature <= 0: at temperature 1, and
  * NaN where that row's largest logit is not finite), 0 for -1.
  * Weights and sums are formed in fp64 from the fp32 logits (relative error below 1e-11), in a fixed order.  1 <= T <= 256.
- * ws: DEVICE, rl_op_verify_drafts_ws_bytes bytes, 8-byte aligned. */
+ * ws: DEVICE, ws_bytes long, 8-byte aligned, at least rl_op_verify_drafts_ws_bytes (else RL_GEN_E_CAPACITY). */
 int rl_op_verify_drafts(const float *target, int64_t ldt, const float *draft, int64_t ldd, const int32_t *drafts, const float *u,
                         const int32_t *d_span, int32_t B, int32_t T, int32_t V, double temperature, int32_t *accepted, int32_t *tokens,
-                        float *logp, void *ws, void *hip_stream);
+                        float *logp, void *ws, size_t ws_bytes, void *hip_stream);
 size_t rl_op_verify_drafts_ws_bytes(int32_t B, int32_t T, int32_t V);
 
 /* Plain device-to-device copy of `bytes` bytes (multiple of 16; 16-byte aligned pointers), 16 bytes per

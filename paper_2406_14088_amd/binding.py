@@ -118,11 +118,11 @@ def lib():
         "rl_op_build_rope_table_scaled": (C.c_int, [vp, i32, i32, f32, i32, f32, i32, f32, f32]),
         "rl_op_rope_append_at": (C.c_int, [vp, i32, sz, i32, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp]),
         "rl_op_span_attention_ws_floats": (sz, [i32, i32, i32, i32, i32, i32, i32, i32]),
-        "rl_op_span_attention": (C.c_int, [vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, vp]),
+        "rl_op_span_attention": (C.c_int, [vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, sz, i32, i32, i32, i32, i32, i32, i32, vp]),
         "rl_op_evict_rows_ws_bytes": (sz, [i32, i32, i32, i32]),
-        "rl_op_evict_rows": (C.c_int, [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp]),
+        "rl_op_evict_rows": (C.c_int, [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, i32, i32, i32, i32, i32, i32, vp]),
         "rl_op_verify_drafts_ws_bytes": (sz, [i32, i32, i32]),
-        "rl_op_verify_drafts": (C.c_int, [vp, i64, vp, i64, vp, vp, vp, i32, i32, i32, C.c_double, vp, vp, vp, vp, vp]),
+        "rl_op_verify_drafts": (C.c_int, [vp, i64, vp, i64, vp, vp, vp, i32, i32, i32, C.c_double, vp, vp, vp, vp, sz, vp]),
         "rl_op_copy": (C.c_int, [vp, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
@@ -197,37 +197,45 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
-def _args_fit(where: str, *specs):
-    """Operands of the span operators: (name, tensor or None, element types, least number of elements).  All on the current GPU,
-    contiguous, of one of the types and long enough, so that no kernel reads or writes outside them."""
-    import torch
-    dev = torch.cuda.current_device()
-    for name, t, types, n in specs:
-        if t is None:
-            continue
-        if t.dtype not in types or not t.is_contiguous() or t.numel() < n or t.get_device() != dev:
-            raise RlGenError(-2, where, f"{name}: expected a contiguous tensor of at least {n} elements of {types[0]} on the current GPU "
-                                        f"(cuda:{dev}), got {t.numel()} of {t.dtype} on {t.device}")
+class _Fit:
+    """Operands of the span operators: all on the current GPU, contiguous, of one of the element types and long enough, so that no kernel
+    reads or writes outside them.  Calling it gives the pointer (None for None)."""
 
+    __slots__ = ("where", "dev")
+    f32 = i32 = h16 = raw = None      # element types
 
-def _span_types():
-    global _SPAN_TYPES
-    if _SPAN_TYPES is None:
+    def __init__(self, where: str):
         import torch
-        _SPAN_TYPES = ((torch.float32,), (torch.int32,), (torch.float16, torch.int16, torch.uint16), (torch.uint8, torch.int64, torch.int32, torch.float32))
-    return _SPAN_TYPES
+        if _Fit.f32 is None:
+            _Fit.i32, _Fit.h16 = (torch.int32,), (torch.float16, torch.int16, torch.uint16)
+            _Fit.raw, _Fit.f32 = (torch.uint8, torch.int64, torch.int32, torch.float32), (torch.float32,)
+        self.where, self.dev = where, torch._C._cuda_getDevice()
 
+    def __call__(self, name: str, t, types, n: int):
+        if t is None:
+            return None
+        if t.dtype in types and t.get_device() == self.dev and t.numel() >= n and t.is_contiguous():
+            return t.data_ptr()
+        raise RlGenError(-2, self.where, f"{name}: expected a contiguous tensor of at least {n} elements of {types[0]} on the current GPU "
+                                         f"(cuda:{self.dev}), got {t.numel()} of {t.dtype} on {t.device}")
 
-_SPAN_TYPES = None
+    def stream(self) -> int:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(self.dev)
 
+    def cache(self, kc, vc, kscale, vscale, table, B: int, Hkv: int, hd: int, S: int):
+        """Pointers of kc, vc, kscale, vscale, table and the stride of the page lists."""
+        rows, pages, stride = B * Hkv * S, None, 0
+        if table is not None:
+            if table.dim() != 2 or table.shape[0] < B:
+                raise RlGenError(-2, self.where, "table: expected int32 [B, pages per sequence]")
+            rows, pages, stride = 0, self("table", table, _Fit.i32, 0), table.shape[1]
+        return (self("kc", kc, _Fit.h16, rows * hd), self("vc", vc, _Fit.h16, rows * hd), self("kscale", kscale, _Fit.f32, rows),
+                self("vscale", vscale, _Fit.f32, rows), pages, stride)
 
-def _page_args(where: str, table, page_size: int, B: int, Hkv: int, S: int, kc):
-    """(table pointer, its stride, rows of kc that the lists or slabs need at least)"""
-    if table is None:
-        return None, 0, B * Hkv * S
-    if table.dim() != 2 or table.shape[0] < B:
-        raise RlGenError(-2, where, "table: expected int32 [B, pages per sequence]")
-    return table.data_ptr(), table.shape[1], 0
+    def check(self, rc: int):
+        if rc != 0:
+            raise RlGenError(rc, self.where)
 
 
 class Generator:
@@ -606,100 +614,96 @@ class _Ops:
         self._ck(lib().rl_op_prefill_attention(q.data_ptr(), kc.data_ptr(), vc.data_ptr(), out.data_ptr(), nb, b0, T, Hq, Hkv,
                                                hd, S, _ptr(kscale), _ptr(vscale), _ptr(out_lo), _ptr(q_lo), _stream()), "rl_op_prefill_attention")
 
-    # -- steps of several tokens over a bounded cache: sizes follow from d_pos / d_len ([B]), T, the heads and S; operands are
-    #    checked for type, layout, device and length
+    # -- steps of several tokens over a bounded cache: B follows from the per-sequence lengths or positions; operands are checked for
+    #    type, layout, device and length
 
     def build_rope_table_scaled(self, tab, n_pos, rot_dim, base, kind=0, factor=1.0, orig_len=0, low=1.0, high=32.0):
-        f32 = _span_types()[0]
-        _args_fit("rl_op_build_rope_table_scaled", ("tab", tab, f32, n_pos * rot_dim))
-        self._ck(lib().rl_op_build_rope_table_scaled(tab.data_ptr(), n_pos, rot_dim, base, kind, factor, orig_len, low, high),
-                 "rl_op_build_rope_table_scaled")
+        fit = _Fit("rl_op_build_rope_table_scaled")
+        fit.check(lib().rl_op_build_rope_table_scaled(fit("tab", tab, fit.f32, n_pos * rot_dim), n_pos, rot_dim, base, kind, factor, orig_len,
+                                                      low, high))
 
     def rope_append_at(self, qkv, nsplit, split_stride, T, d_pos, d_slot, rope_tab, rope_style, rot_dim, Hq, Hkv, hd, S, kc, vc, q_f32=None,
                        q_f16=None, q_f16_lo=None, d_span=None, kscale=None, vscale=None, table=None, page_size=0, weight=None, row_pos=None):
-        """qkv fp32 [nsplit, B*T, (Hq+2Hkv)*hd] (partials split_stride elements apart); rope_tab fp32 [positions, rot_dim/2, 2]."""
-        name = "rl_op_rope_append_at"
-        f32, i32, h16, _ = _span_types()
+        """qkv fp32 [nsplit, B*T, (Hq+2Hkv)*hd] (partials split_stride elements apart); rope_tab fp32 [positions, rot_dim/2, 2]; d_pos, d_slot
+        int32 [B]."""
+        fit = _Fit("rl_op_rope_append_at")
+        f32, i32, h16 = fit.f32, fit.i32, fit.h16
         B = d_pos.numel()
-        M, width = B * T, (Hq + 2 * Hkv) * hd
-        tp, ts, rows = _page_args(name, table, page_size, B, Hkv, S, kc)
-        _args_fit(name, ("qkv", qkv, f32, (nsplit - 1) * split_stride + M * width), ("d_pos", d_pos, i32, B), ("d_slot", d_slot, i32, B),
-                  ("d_span", d_span, i32, B), ("rope_tab", rope_tab, f32, rot_dim), ("kc", kc, h16, rows * hd), ("vc", vc, h16, rows * hd),
-                  ("kscale", kscale, f32, rows), ("vscale", vscale, f32, rows), ("table", table, i32, 0), ("q_f32", q_f32, f32, M * Hq * hd),
-                  ("q_f16", q_f16, h16, M * Hq * hd), ("q_f16_lo", q_f16_lo, h16, M * Hq * hd), ("weight", weight, f32, B * Hkv * S),
-                  ("row_pos", row_pos, i32, B * Hkv * S))
         if B == 0:
             return
-        self._ck(lib().rl_op_rope_append_at(qkv.data_ptr(), nsplit, split_stride, B, T, d_pos.data_ptr(), d_slot.data_ptr(), _ptr(d_span),
-                                            rope_tab.data_ptr(), rope_tab.numel() // max(rot_dim, 1), rope_style, rot_dim, Hq, Hkv, hd, S, _ptr(q_f32),
-                                            _ptr(q_f16), _ptr(q_f16_lo), kc.data_ptr(), vc.data_ptr(), _ptr(kscale), _ptr(vscale), tp, ts,
-                                            page_size, _ptr(weight), _ptr(row_pos), _stream()), name)
+        n, side = B * T * Hq * hd, B * Hkv * S
+        k, v, ks, vs, pages, stride = fit.cache(kc, vc, kscale, vscale, table, B, Hkv, hd, S)
+        fit.check(lib().rl_op_rope_append_at(fit("qkv", qkv, f32, (nsplit - 1) * split_stride + B * T * (Hq + 2 * Hkv) * hd), nsplit, split_stride,
+                                             B, T, fit("d_pos", d_pos, i32, B), fit("d_slot", d_slot, i32, B), fit("d_span", d_span, i32, B),
+                                             fit("rope_tab", rope_tab, f32, rot_dim), rope_tab.numel() // max(rot_dim, 1), rope_style, rot_dim, Hq, Hkv,
+                                             hd, S, fit("q_f32", q_f32, f32, n), fit("q_f16", q_f16, h16, n), fit("q_f16_lo", q_f16_lo, h16, n), k, v,
+                                             ks, vs, pages, stride, page_size, fit("weight", weight, f32, side), fit("row_pos", row_pos, i32, side),
+                                             fit.stream()))
 
     def span_attention_ws_floats(self, B, T, Hq, Hkv, hd, S, nsplit, weights):
         return int(lib().rl_op_span_attention_ws_floats(B, T, Hq, Hkv, hd, S, nsplit, int(bool(weights))))
 
     def span_attention(self, q, kc, vc, d_len, out, ws, T, Hq, Hkv, hd, S, nsplit=0, d_span=None, kscale=None, vscale=None, out_lo=None,
                        weight=None, table=None, page_size=0):
-        """q fp32 [B*T, Hq*hd]; ws fp32 [span_attention_ws_floats(...)] or None when that is 0; weight fp32 [B, Hkv, S] is added to."""
-        name = "rl_op_span_attention"
-        f32, i32, h16, _ = _span_types()
+        """q fp32 [B*T, Hq*hd]; d_len int32 [B]; ws fp32 [span_attention_ws_floats(...)] or None when that is 0; weight fp32 [B, Hkv, S] is
+        added to."""
+        fit = _Fit("rl_op_span_attention")
+        f32, i32, h16 = fit.f32, fit.i32, fit.h16
         B = d_len.numel()
-        n = B * T * Hq * hd
-        tp, ts, rows = _page_args(name, table, page_size, B, Hkv, S, kc)
-        _args_fit(name, ("q", q, f32, n), ("kc", kc, h16, rows * hd), ("vc", vc, h16, rows * hd), ("kscale", kscale, f32, rows),
-                  ("vscale", vscale, f32, rows), ("table", table, i32, 0), ("d_len", d_len, i32, B), ("d_span", d_span, i32, B),
-                  ("out", out, h16, n), ("out_lo", out_lo, h16, n), ("weight", weight, f32, B * Hkv * S),
-                  ("ws", ws, f32, lib().rl_op_span_attention_ws_floats(B, T, Hq, Hkv, hd, S, nsplit, int(weight is not None))))
         if B == 0:
             return
-        self._ck(lib().rl_op_span_attention(q.data_ptr(), kc.data_ptr(), vc.data_ptr(), _ptr(kscale), _ptr(vscale), tp, ts, page_size,
-                                            d_len.data_ptr(), _ptr(d_span), out.data_ptr(), _ptr(out_lo), _ptr(weight), _ptr(ws), B, T, Hq, Hkv,
-                                            hd, S, nsplit, _stream()), name)
+        n = B * T * Hq * hd
+        k, v, ks, vs, pages, stride = fit.cache(kc, vc, kscale, vscale, table, B, Hkv, hd, S)
+        fit.check(lib().rl_op_span_attention(fit("q", q, f32, n), k, v, ks, vs, pages, stride, page_size, fit("d_len", d_len, i32, B),
+                                             fit("d_span", d_span, i32, B), fit("out", out, h16, n), fit("out_lo", out_lo, h16, n),
+                                             fit("weight", weight, f32, B * Hkv * S), fit("ws", ws, f32, 0), 0 if ws is None else ws.numel(), B, T, Hq,
+                                             Hkv, hd, S, nsplit, fit.stream()))
 
     def evict_rows_ws_bytes(self, B, Hkv, S, keep):
         return int(lib().rl_op_evict_rows_ws_bytes(B, Hkv, S, keep))
 
     def evict_rows(self, kc, vc, weight, weight_out, d_len, d_len_out, ws, Hkv, hd, S, keep, recent, pos=None, pos_out=None, kscale=None,
                    vscale=None, table=None, page_size=0):
-        """weight / pos [B, Hkv, S]; ws: evict_rows_ws_bytes(...) bytes; d_len_out may be None."""
-        name = "rl_op_evict_rows"
-        f32, i32, h16, raw = _span_types()
+        """weight / pos [B, Hkv, S]; d_len int32 [B]; ws: evict_rows_ws_bytes(...) bytes; d_len_out may be None."""
+        fit = _Fit("rl_op_evict_rows")
+        f32, i32 = fit.f32, fit.i32
         B = d_len.numel()
-        tp, ts, rows = _page_args(name, table, page_size, B, Hkv, S, kc)
-        need = lib().rl_op_evict_rows_ws_bytes(B, Hkv, S, keep)
-        _args_fit(name, ("kc", kc, h16, rows * hd), ("vc", vc, h16, rows * hd), ("kscale", kscale, f32, rows), ("vscale", vscale, f32, rows),
-                  ("table", table, i32, 0), ("weight", weight, f32, B * Hkv * S), ("weight_out", weight_out, f32, B * Hkv * S),
-                  ("pos", pos, i32, B * Hkv * S), ("pos_out", pos_out, i32, B * Hkv * S), ("d_len", d_len, i32, B),
-                  ("d_len_out", d_len_out, i32, B), ("ws", ws, raw, -(-need // ws.element_size())))
         if B == 0:
             return
-        self._ck(lib().rl_op_evict_rows(kc.data_ptr(), vc.data_ptr(), _ptr(kscale), _ptr(vscale), tp, ts, page_size, weight.data_ptr(),
-                                        weight_out.data_ptr(), _ptr(pos), _ptr(pos_out), d_len.data_ptr(), _ptr(d_len_out), ws.data_ptr(), B,
-                                        Hkv, hd, S, keep, recent, _stream()), name)
+        side = B * Hkv * S
+        k, v, ks, vs, pages, stride = fit.cache(kc, vc, kscale, vscale, table, B, Hkv, hd, S)
+        fit.check(lib().rl_op_evict_rows(k, v, ks, vs, pages, stride, page_size, fit("weight", weight, f32, side),
+                                         fit("weight_out", weight_out, f32, side), fit("pos", pos, i32, side), fit("pos_out", pos_out, i32, side),
+                                         fit("d_len", d_len, i32, B), fit("d_len_out", d_len_out, i32, B), fit("ws", ws, fit.raw, 0),
+                                         ws.numel() * ws.element_size(), B, Hkv, hd, S, keep, recent, fit.stream()))
 
     def verify_drafts_ws_bytes(self, B, T, V):
         return int(lib().rl_op_verify_drafts_ws_bytes(B, T, V))
 
     def verify_drafts(self, target, drafts, u, accepted, tokens, ws, temperature, draft=None, d_span=None, logp=None):
         """target fp32 [B*(T+1), V], draft fp32 [B*T, V] or None (both may have rows further apart than V); drafts int32 [B, T]; u fp32
-        [B, T+1] (None when temperature <= 0); accepted int32 [B]; tokens int32, logp fp32 [B, T+1]."""
-        name = "rl_op_verify_drafts"
-        f32, i32, _, raw = _span_types()
+        [B, T+1] (None when temperature <= 0); accepted int32 [B]; tokens int32, logp fp32 [B, T+1]; ws: verify_drafts_ws_bytes(...)."""
+        fit = _Fit("rl_op_verify_drafts")
+        f32, i32 = fit.f32, fit.i32
         B, T = drafts.shape
-        V = target.shape[1]
-        ld = []
-        for what, x, rows in (("target", target, B * (T + 1)), ("draft", draft, B * T)):
-            if x is not None and (x.dim() != 2 or x.shape[0] < rows or x.shape[1] != V or x.stride(1) != 1 or x.dtype not in f32 or
-                                  x.get_device() != drafts.get_device()):
-                raise RlGenError(-2, name, f"{what}: expected fp32 [{rows}, {V}] with consecutive columns, got {tuple(x.shape)} of {x.dtype}")
-            ld.append(V if x is None or x.shape[0] <= 1 else x.stride(0))
-        _args_fit(name, ("drafts", drafts, i32, B * T), ("u", u, f32, B * (T + 1)), ("d_span", d_span, i32, B), ("accepted", accepted, i32, B),
-                  ("tokens", tokens, i32, B * (T + 1)), ("logp", logp, f32, B * (T + 1)),
-                  ("ws", ws, raw, -(-lib().rl_op_verify_drafts_ws_bytes(B, T, V) // ws.element_size())))
         if B == 0:
             return
-        self._ck(lib().rl_op_verify_drafts(target.data_ptr(), ld[0], _ptr(draft), ld[1], drafts.data_ptr(), _ptr(u), _ptr(d_span), B, T, V,
-                                           float(temperature), accepted.data_ptr(), tokens.data_ptr(), _ptr(logp), ws.data_ptr(), _stream()), name)
+        V = target.shape[1]
+
+        def rows(name, x, count):       # pointer and distance of consecutive rows
+            if x is None:
+                return None, V
+            if x.dim() != 2 or x.shape[0] < count or x.shape[1] != V or x.stride(1) != 1 or x.dtype not in f32 or x.get_device() != fit.dev:
+                raise RlGenError(-2, fit.where, f"{name}: expected fp32 [{count}, {V}] with consecutive columns on cuda:{fit.dev}, got "
+                                                f"{tuple(x.shape)} of {x.dtype} on {x.device}")
+            return x.data_ptr(), (V if x.shape[0] == 1 else x.stride(0))
+
+        tp, ldt = rows("target", target, B * (T + 1))
+        dp, ldd = rows("draft", draft, B * T)
+        fit.check(lib().rl_op_verify_drafts(tp, ldt, dp, ldd, fit("drafts", drafts, i32, B * T), fit("u", u, f32, B * (T + 1)),
+                                            fit("d_span", d_span, i32, B), B, T, V, float(temperature), fit("accepted", accepted, i32, B),
+                                            fit("tokens", tokens, i32, B * (T + 1)), fit("logp", logp, f32, B * (T + 1)), fit("ws", ws, fit.raw, 0),
+                                            ws.numel() * ws.element_size(), fit.stream()))
 
     def sample(self, logits, temperature, u, nxt):
         B, V = logits.shape

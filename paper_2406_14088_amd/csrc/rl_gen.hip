@@ -1784,15 +1784,17 @@ size_t rl_op_span_attention_ws_floats(int32_t B, int32_t T, int32_t Hq, int32_t 
 
 int rl_op_span_attention(const float *q, const uint16_t *kc, const uint16_t *vc, const float *kscale, const float *vscale,
                          const int32_t *table, int32_t table_stride, int32_t page_size, const int32_t *d_len, const int32_t *d_span,
-                         uint16_t *out, uint16_t *out_lo, float *weight, float *ws, int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd,
-                         int32_t S, int32_t nsplit, void *st) {
+                         uint16_t *out, uint16_t *out_lo, float *weight, float *ws, size_t ws_floats, int32_t B, int32_t T, int32_t Hq,
+                         int32_t Hkv, int32_t hd, int32_t S, int32_t nsplit, void *st) {
     if (!q || !d_len || !out) return RL_GEN_E_NULL;
     SpanArgs a;
     if (int rc = span_cache_map(kc, vc, kscale, vscale, table, table_stride, page_size, B, Hkv, hd, S, &a.map)) return rc;
     if (!span_shape_ok(B, T, Hq, Hkv, hd, S, nsplit)) return RL_GEN_E_SHAPE;
     if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)out_lo | (uintptr_t)ws) % 16) return RL_GEN_E_SHAPE;
     a.nsplit = nsplit ? nsplit : span_attention_splits(B, T, Hq, Hkv, hd, S);
-    if (!ws && span_attention_ws_floats(B, T, Hq, Hkv, hd, S, a.nsplit, weight != nullptr) > 0) return RL_GEN_E_NULL;
+    const size_t need = span_attention_ws_floats(B, T, Hq, Hkv, hd, S, a.nsplit, weight != nullptr);
+    if (!ws && need > 0) return RL_GEN_E_NULL;
+    if (need > ws_floats) return RL_GEN_E_CAPACITY;
     a.q = q; a.kc = kc; a.vc = vc; a.d_len = d_len; a.d_span = d_span; a.out = out; a.out_lo = out_lo; a.weight = weight; a.ws = ws;
     a.B = B; a.T = T; a.Hq = Hq; a.Hkv = Hkv; a.hd = hd; a.S = S;
     launch_span_attention(a, reinterpret_cast<hipStream_t>(st));
@@ -1806,11 +1808,13 @@ size_t rl_op_evict_rows_ws_bytes(int32_t B, int32_t Hkv, int32_t S, int32_t keep
 
 int rl_op_evict_rows(uint16_t *kc, uint16_t *vc, float *kscale, float *vscale, const int32_t *table, int32_t table_stride,
                      int32_t page_size, const float *weight, float *weight_out, const int32_t *pos, int32_t *pos_out, const int32_t *d_len,
-                     int32_t *d_len_out, void *ws, int32_t B, int32_t Hkv, int32_t hd, int32_t S, int32_t keep, int32_t recent, void *st) {
+                     int32_t *d_len_out, void *ws, size_t ws_bytes, int32_t B, int32_t Hkv, int32_t hd, int32_t S, int32_t keep,
+                     int32_t recent, void *st) {
     if (!weight || !weight_out || (pos && !pos_out) || !d_len || !ws) return RL_GEN_E_NULL;
     EvictArgs a;
     if (int rc = span_cache_map(kc, vc, kscale, vscale, table, table_stride, page_size, B, Hkv, hd, S, &a.map)) return rc;
     if (keep < 1 || keep > S || recent < 0 || recent > keep || (uintptr_t)ws % 8) return RL_GEN_E_SHAPE;
+    if (ws_bytes < evict_rows_ws_bytes(B, Hkv, S, keep)) return RL_GEN_E_CAPACITY;
     a.kc = kc; a.vc = vc; a.weight = weight; a.weight_out = weight_out; a.pos = pos; a.pos_out = pos ? pos_out : nullptr;
     a.d_len = d_len; a.d_len_out = d_len_out; a.moves = reinterpret_cast<int32_t *>(ws);
     a.B = B; a.Hkv = Hkv; a.hd = hd; a.S = S; a.keep = keep; a.recent = recent; a.max_moves = 0;
@@ -1826,11 +1830,12 @@ size_t rl_op_verify_drafts_ws_bytes(int32_t B, int32_t T, int32_t V) { return ve
 
 int rl_op_verify_drafts(const float *target, int64_t ldt, const float *draft, int64_t ldd, const int32_t *drafts, const float *u,
                         const int32_t *d_span, int32_t B, int32_t T, int32_t V, double temperature, int32_t *accepted, int32_t *tokens,
-                        float *logp, void *ws, void *st) {
+                        float *logp, void *ws, size_t ws_bytes, void *st) {
     const bool sampled = temperature > 0;
     if (!target || !drafts || !accepted || !tokens || !ws || (sampled && !u)) return RL_GEN_E_NULL;
     if (!verify_shape_ok(B, T, V) || ldt < V || (sampled && draft && ldd < V) || (uintptr_t)ws % 8) return RL_GEN_E_SHAPE;
     if (temperature != temperature || temperature > 1e300 || (sampled && temperature < 1e-30)) return RL_GEN_E_SHAPE;
+    if (ws_bytes < verify_drafts_ws_bytes(B, T, V)) return RL_GEN_E_CAPACITY;
     VerifyArgs a;
     a.target = target; a.ldt = ldt; a.draft = sampled ? draft : nullptr; a.ldd = ldd; a.drafts = drafts; a.u = u; a.d_span = d_span;
     a.B = B; a.T = T; a.V = V; a.temperature = temperature; a.accepted = accepted; a.tokens = tokens; a.logp = logp; a.ws = ws;

@@ -3,7 +3,7 @@ import ctypes as C
 
 import pytest
 
-E_NULL, E_SHAPE = -1, -2
+E_NULL, E_SHAPE, E_CAPACITY = -1, -2, -3
 P = 4096            # an aligned address that is never read
 
 
@@ -21,21 +21,21 @@ def _append(L, **kw):
 
 
 def _span(L, **kw):
-    a = dict(q=P, kc=P, vc=P, ks=None, vs=None, table=None, ts=0, page=0, len=P, span=None, out=P, lo=None, w=None, ws=None, B=2, T=3, Hq=4, Hkv=2, hd=64,
+    a = dict(q=P, kc=P, vc=P, ks=None, vs=None, table=None, ts=0, page=0, len=P, span=None, out=P, lo=None, w=None, ws=None, wsn=0, B=2, T=3, Hq=4, Hkv=2, hd=64,
              S=32, nsplit=1, st=None)
     assert set(kw) <= set(a)
     return L.rl_op_span_attention(*{**a, **kw}.values())
 
 
 def _evict(L, **kw):
-    a = dict(kc=P, vc=P, ks=None, vs=None, table=None, ts=0, page=0, w=P, wo=P, pos=None, po=None, len=P, lo=None, ws=P, B=2, Hkv=2, hd=64, S=32, keep=16,
+    a = dict(kc=P, vc=P, ks=None, vs=None, table=None, ts=0, page=0, w=P, wo=P, pos=None, po=None, len=P, lo=None, ws=P, wsn=1 << 20, B=2, Hkv=2, hd=64, S=32, keep=16,
              recent=4, st=None)
     assert set(kw) <= set(a)
     return L.rl_op_evict_rows(*{**a, **kw}.values())
 
 
 def _verify(L, **kw):
-    a = dict(t=P, ldt=100, d=None, ldd=0, drafts=P, u=P, span=None, B=2, T=3, V=100, temp=1.0, acc=P, tok=P, lp=None, ws=P, st=None)
+    a = dict(t=P, ldt=100, d=None, ldd=0, drafts=P, u=P, span=None, B=2, T=3, V=100, temp=1.0, acc=P, tok=P, lp=None, ws=P, wsn=1 << 20, st=None)
     assert set(kw) <= set(a)
     return L.rl_op_verify_drafts(*{**a, **kw}.values())
 
@@ -57,6 +57,10 @@ def test_operands_that_go_together(L):
         assert call(L, kc=P + 2) == E_SHAPE and call(L, vc=P + 8) == E_SHAPE
     assert _append(L, ql=P) == E_NULL and _evict(L, pos=P) == E_NULL
     assert _span(L, w=P) == E_NULL                                 # weights need a workspace
+    assert _span(L, w=P, ws=P, wsn=L.rl_op_span_attention_ws_floats(2, 3, 4, 2, 64, 32, 1, 1) - 1) == E_CAPACITY
+    assert _span(L, ws=P, nsplit=2, wsn=L.rl_op_span_attention_ws_floats(2, 3, 4, 2, 64, 32, 2, 0) - 1) == E_CAPACITY
+    assert _evict(L, wsn=L.rl_op_evict_rows_ws_bytes(2, 2, 32, 16) - 1) == E_CAPACITY
+    assert _verify(L, wsn=L.rl_op_verify_drafts_ws_bytes(2, 3, 100) - 1) == E_CAPACITY
 
 
 def test_sizes_and_options(L):
