@@ -1,61 +1,101 @@
 // Rotary embedding and cache append of a span of new tokens at given positions and slots (rl_op_rope_append_at): part of a head
 // or all of it, neighbouring or half-split pairs, the cache half or block-scaled, contiguous or paged.
+//
+// A stream: every value of the projection (nsplit fp32 partials) is read once, q and the cache rows are written once.  A thread takes 8
+// elements of a head -- four pairs, or 8 neighbours of the part that does not rotate -- as two 16-byte loads per partial, issued before the
+// positions are known, so that the chain of latencies is positions -> table -> stores.  8 or 16 consecutive lanes hold a head: the
+// maximum of a block-scaled row is a reduction among them.
 #include "kernels.h"
 
-// One thread per pair of elements; a head is hd / 2 consecutive lanes, so the maximum of a block-scaled row is a shuffle reduction.
+template <bool SCALED>
 __global__ __launch_bounds__(256) void rope_append_at_kernel(RopeAppendAtArgs a) {
-    const int m = blockIdx.x, b = m / a.T, t = m % a.T;
-    if (a.d_span && t >= a.d_span[b]) return;
-    const long pos = (long)a.d_pos[b] + t, slot = (long)a.d_slot[b] + t;
-    if (pos < 0 || pos >= a.tab_rows || slot < 0 || slot >= a.S) return;
-    const int hd = a.hd, half = hd >> 1, rh = a.rot_dim >> 1;
-    const int it = blockIdx.y * 256 + threadIdx.x;
-    const int head = it / half, r = it % half;
+    const int m = blockIdx.x, b = m / a.T, t = m % a.T, hd = a.hd;
+    const int lph = hd >> 3, sh = hd == 128 ? 4 : 3;  // threads of a head
+    const int it = blockIdx.y * 256 + threadIdx.x, head = it >> sh, u = it & (lph - 1);
     const int heads = a.Hq + 2 * a.Hkv;
     const bool valid = head < heads;
     const int kind = head < a.Hq ? 0 : (head < a.Hq + a.Hkv ? 1 : 2);
-    const int kvh = kind == 0 ? 0 : (head - a.Hq) % a.Hkv;
-    // pair r of a head: the first rot_dim / 2 pairs rotate, the others are neighbours behind them
-    int ia = 2 * r, ib = 2 * r + 1;
-    if (r < rh && a.rope_style == 1) { ia = r; ib = r + rh; }
-    float x = 0.f, y = 0.f;
+    // first and second group of four elements: elements that pair up with each other in style 1, neighbours otherwise
+    const int rh = a.rot_dim >> 1;
+    const bool turns = kind != 2 && 8 * u < a.rot_dim, halves = a.rope_style == 1 && 8 * u < a.rot_dim;
+    const int e0 = halves ? 4 * u : 8 * u, e1 = halves ? 4 * u + rh : 8 * u + 4;
+    f32x4_t x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
     if (valid) {
-        const float *row = a.qkv + (size_t)m * heads * hd + (size_t)head * hd;
-        for (int s = 0; s < a.nsplit; ++s) {
-            x += row[s * a.split_stride + ia];
-            y += row[s * a.split_stride + ib];
+        const float *row = a.qkv + ((size_t)m * heads + head) * hd;
+        x = *reinterpret_cast<const f32x4_t *>(row + e0);
+        y = *reinterpret_cast<const f32x4_t *>(row + e1);
+        for (int s = 1; s < a.nsplit; ++s) {
+            x += *reinterpret_cast<const f32x4_t *>(row + s * a.split_stride + e0);
+            y += *reinterpret_cast<const f32x4_t *>(row + s * a.split_stride + e1);
         }
-        if (kind != 2 && r < rh) {
-            const float *cs = a.rope_tab + (size_t)pos * a.rot_dim + 2 * r;
-            const float xr = x * cs[0] - y * cs[1], yr = x * cs[1] + y * cs[0];
-            x = xr; y = yr;
-        }
-        if (kind == 0) {
-            const size_t o = ((size_t)m * a.Hq + head) * hd;
-            if (a.q_f32) { a.q_f32[o + ia] = x; a.q_f32[o + ib] = y; }
-            if (a.q_f16) {
-                const f16_t hx = f32_to_f16(x), hy = f32_to_f16(y);
-                a.q_f16[o + ia] = hx; a.q_f16[o + ib] = hy;
-                if (a.q_f16_lo) { a.q_f16_lo[o + ia] = f32_to_f16(x - f16_to_f32(hx)); a.q_f16_lo[o + ib] = f32_to_f16(y - f16_to_f32(hy)); }
+    }
+    if (a.d_span && t >= a.d_span[b]) return;
+    const int64_t pos = (int64_t)a.d_pos[b] + t, slot = (int64_t)a.d_slot[b] + t;
+    if (pos < 0 || pos >= a.tab_rows || slot < 0 || slot >= a.S) return;
+    if (valid && turns) {
+        const float *cs = a.rope_tab + (size_t)pos * a.rot_dim + 8 * u;  // (cos, sin) of pairs 4 u .. 4 u + 3
+        const f32x4_t c0 = *reinterpret_cast<const f32x4_t *>(cs), c1 = *reinterpret_cast<const f32x4_t *>(cs + 4);
+        const float co[4] = {c0.x, c0.z, c1.x, c1.z}, si[4] = {c0.y, c0.w, c1.y, c1.w};
+        if (halves) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p = x[i], q = y[i];
+                x[i] = __builtin_fmaf(p, co[i], -(q * si[i]));  // the roundings of rope_append_kernel
+                y[i] = __builtin_fmaf(q, co[i], p * si[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float p = x[2 * i], q = x[2 * i + 1], r = y[2 * i], s = y[2 * i + 1];
+                x[2 * i] = __builtin_fmaf(p, co[i], -(q * si[i]));
+                x[2 * i + 1] = __builtin_fmaf(q, co[i], p * si[i]);
+                y[2 * i] = __builtin_fmaf(r, co[2 + i], -(s * si[2 + i]));
+                y[2 * i + 1] = __builtin_fmaf(s, co[2 + i], r * si[2 + i]);
             }
         }
     }
-    float am = kind != 0 ? fmaxf(fabsf(x), fabsf(y)) : 0.f;
-    if (a.map.kscale)
-        for (int o = 1; o < half; o <<= 1) am = fmaxf(am, __shfl_xor(am, o, 64));
-    if (!valid || kind == 0) return;
+    float am = 0.f;
+    if (SCALED) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) am = fmaxf(am, fmaxf(fabsf(x[i]), fabsf(y[i])));
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) am = fmaxf(am, __shfl_xor(am, o, 64));
+        if (hd == 128) am = fmaxf(am, __shfl_xor(am, 8, 64));
+    }
+    if (!valid) return;
+    if (kind == 0) {
+        const size_t o = ((size_t)m * a.Hq + head) * hd;
+        if (a.q_f32) {
+            *reinterpret_cast<f32x4_t *>(a.q_f32 + o + e0) = x;
+            *reinterpret_cast<f32x4_t *>(a.q_f32 + o + e1) = y;
+        }
+        if (a.q_f16) {
+            const u32x2_t hx = {pack_f16x2(x.x, x.y), pack_f16x2(x.z, x.w)}, hy = {pack_f16x2(y.x, y.y), pack_f16x2(y.z, y.w)};
+            *reinterpret_cast<u32x2_t *>(a.q_f16 + o + e0) = hx;
+            *reinterpret_cast<u32x2_t *>(a.q_f16 + o + e1) = hy;
+            if (a.q_f16_lo) {
+                *reinterpret_cast<u32x2_t *>(a.q_f16_lo + o + e0) = u32x2_t{pack_f16x2_lo(x.x, x.y, hx.x), pack_f16x2_lo(x.z, x.w, hx.y)};
+                *reinterpret_cast<u32x2_t *>(a.q_f16_lo + o + e1) = u32x2_t{pack_f16x2_lo(y.x, y.y, hy.x), pack_f16x2_lo(y.z, y.w, hy.y)};
+            }
+        }
+        return;
+    }
+    const int kvh = kind == 1 ? head - a.Hq : head - a.Hq - a.Hkv;
     const size_t rowi = kv_row_index(a.map, b, kvh, a.Hkv, a.S, (int)slot);
     f16_t *dst = (kind == 1 ? a.kc : a.vc) + rowi * hd;
-    if (a.map.kscale) {
+    u32x2_t hx, hy;
+    if (SCALED) {
         const float inv = kv_inv_of(am);
-        dst[ia] = (f16_t)(kv_quant(x, inv) & 0xffff);
-        dst[ib] = (f16_t)(kv_quant(y, inv) & 0xffff);
-        if (r == 0) (kind == 1 ? a.map.kscale : a.map.vscale)[rowi] = kv_scale_of(am);
+        hx = u32x2_t{pack_i16x2(kv_quant(x.x, inv), kv_quant(x.y, inv)), pack_i16x2(kv_quant(x.z, inv), kv_quant(x.w, inv))};
+        hy = u32x2_t{pack_i16x2(kv_quant(y.x, inv), kv_quant(y.y, inv)), pack_i16x2(kv_quant(y.z, inv), kv_quant(y.w, inv))};
+        if (u == 0) (kind == 1 ? a.map.kscale : a.map.vscale)[rowi] = kv_scale_of(am);
     } else {
-        dst[ia] = f32_to_f16(x);
-        dst[ib] = f32_to_f16(y);
+        hx = u32x2_t{pack_f16x2(x.x, x.y), pack_f16x2(x.z, x.w)};
+        hy = u32x2_t{pack_f16x2(y.x, y.y), pack_f16x2(y.z, y.w)};
     }
-    if (kind == 1 && r == 0) {
+    *reinterpret_cast<u32x2_t *>(dst + e0) = hx;
+    *reinterpret_cast<u32x2_t *>(dst + e1) = hy;
+    if (kind == 1 && u == 0) {
         const size_t w = ((size_t)b * a.Hkv + kvh) * a.S + slot;
         if (a.weight) a.weight[w] = 0.f;
         if (a.row_pos) a.row_pos[w] = (int32_t)pos;
@@ -64,5 +104,7 @@ __global__ __launch_bounds__(256) void rope_append_at_kernel(RopeAppendAtArgs a)
 
 void launch_rope_append_at(const RopeAppendAtArgs &a, hipStream_t st) {
     if (a.B <= 0) return;
-    rope_append_at_kernel<<<dim3(a.B * a.T, ceil_div((a.Hq + 2 * a.Hkv) * (a.hd / 2), 256)), 256, 0, st>>>(a);
+    const dim3 grid(a.B * a.T, ceil_div((a.Hq + 2 * a.Hkv) * (a.hd / 8), 256));
+    if (a.map.kscale) rope_append_at_kernel<true><<<grid, 256, 0, st>>>(a);
+    else rope_append_at_kernel<false><<<grid, 256, 0, st>>>(a);
 }
