@@ -7,12 +7,12 @@
 // A draw may land next to a border of the cumulative distribution, and a vocabulary of V tokens has V of them: weights with a
 // relative error e move a draw to a neighbour with a probability of the order of V * e, about one in a hundred for fp32 (1e-7) and
 // V = 128256.  So weights and sums are fp64: 2^g by rounding g to an integer with an addition, a polynomial of degree 8 (relative error
-// 1.1e-12 on [-1/2, 1/2]; interpolation at the Chebyshev nodes) and an addition to the exponent: 17 instructions per logit.  fp64
+// 1.1e-12 on [-1/2, 1/2]; interpolation at the Chebyshev nodes) and an addition to the exponent: 16 instructions per logit.  fp64
 // multiply-adds run at the rate of unpacked fp32 ones here, so the rows stay a stream from HBM.
 #include "kernels.h"
 
 #define VD_THREADS 256
-#define VD_PICK_THREADS 1024
+#define VD_PICK_THREADS 256
 
 __device__ __forceinline__ double vd_wave_sum(double v) {
 #pragma unroll
@@ -20,11 +20,11 @@ __device__ __forceinline__ double vd_wave_sum(double v) {
     return v;
 }
 
-// 2^g for -1020 <= g <= 1000.
-__device__ __forceinline__ double vd_exp2(double g) {
+// exp(d / temperature) with c = log2(e) / temperature, for -1020 <= d c <= 1000.
+__device__ __forceinline__ double vd_exp(double d, double c) {
     const double magic = 6755399441055744.0;  // 1.5 * 2^52: adding it leaves the nearest integer in the low bits
-    const double t = g + magic;
-    const double f = g - (t - magic);
+    const double t = __builtin_fma(d, c, magic);
+    const double f = __builtin_fma(d, c, -(t - magic));
     double p = 1.3255224878668817e-06;
     p = __builtin_fma(p, f, 1.5310079402249296e-05);
     p = __builtin_fma(p, f, 0.00015403455852453838);
@@ -36,11 +36,11 @@ __device__ __forceinline__ double vd_exp2(double g) {
     p = __builtin_fma(p, f, 1.0);
     return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
 }
-// exp((x - m) / temperature) with c = log2(e) / temperature; 0 below 2^-1020 (and for x = -inf), which no sum notices.
+// exp((x - m) / temperature); 0 where it is below 2^-1020 (and for x = -inf), which no sum notices.
 __device__ __forceinline__ double vd_weight(float x, double m, double c) {
-    const double g = ((double)x - m) * c;
-    const double w = vd_exp2(__builtin_fmax(g, -1020.0));
-    return g >= -1020.0 ? w : 0.0;
+    const double d = (double)x - m, least = -1020.0 / c;
+    const double w = vd_exp(__builtin_fmax(d, least), c);
+    return d >= least ? w : 0.0;
 }
 
 // Workspace: per (sequence, row, chunk) sum, maximum and index of the maximum (-1: the chunk holds a NaN); per sequence and target
@@ -76,27 +76,26 @@ __device__ __forceinline__ const float *vd_row(const VerifyArgs &a, int b, int r
     return r <= a.T ? a.target + ((size_t)b * (a.T + 1) + r) * a.ldt : a.draft + ((size_t)b * a.T + (r - a.T - 1)) * a.ldd;
 }
 
-// One workgroup per (row, chunk of 256 * EPT logits): the logits stay in registers between the maximum and the weights.  A wavefront's weights
-// refer to its own maximum (no barrier before them); the four wavefronts join at the end.  SUMS: off where only the largest is wanted.
-template <int EPT, bool SUMS>
-__global__ __launch_bounds__(VD_THREADS) void vd_rows_kernel(VerifyArgs a, int chunks, int rows) {
-    __shared__ double s_sum[4];
-    __shared__ float s_max[4];
-    __shared__ int s_arg[4];
-    const int chunk = blockIdx.x % chunks, cell_row = blockIdx.x / chunks, r = cell_row % rows, b = cell_row / rows;
+// One wavefront per (row, chunk of 64 * EPT logits), four chunks of a row per workgroup: the logits stay in registers between the maximum and the weights, which refer to the
+// chunk's own maximum.  SUMS, ARG: whether the sum and the index of the maximum are wanted (sampled: sums; greedy: the index, and sums for
+// log-probabilities).
+template <int EPT, bool SUMS, bool ARG>
+__global__ __launch_bounds__(VD_THREADS, 8) void vd_rows_kernel(VerifyArgs a, int chunks, int rows, int groups) {
+    const unsigned id = blockIdx.x / groups;
+    const int chunk = (int)(blockIdx.x % groups) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int r = (int)(id % rows), b = (int)(id / rows);
+    if (chunk >= chunks) return;
     const int n = vd_span(a, b);
     if (r <= a.T ? r > n : r - a.T - 1 >= n) return;  // not reached in any case
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const float *row = vd_row(a, b, r);
-    const int first = chunk * (VD_THREADS * EPT);
-    const int left = a.V - first < VD_THREADS * EPT ? a.V - first : VD_THREADS * EPT;
-    row += first;
+    const int first = chunk * (64 * EPT);
+    const int left = a.V - first < 64 * EPT ? a.V - first : 64 * EPT;
+    const float *row = vd_row(a, b, r) + first;
     float x[EPT];
-    // element e of the thread: index 4 * (tid + 256 * (e / 4)) + e % 4, whole vectors where row and length allow them
+    // element e of the lane: index 4 * (lane + 64 * (e / 4)) + e % 4, whole vectors where row and length allow them
     if ((reinterpret_cast<uintptr_t>(row) & 15) == 0) {
 #pragma unroll
         for (int k = 0; k < EPT / 4; ++k) {
-            const int i = 4 * (tid + VD_THREADS * k);
+            const int i = 4 * (lane + 64 * k);
             f32x4_t v = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
             if (i + 4 <= left) {
                 v = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t *>(row + i));
@@ -111,7 +110,7 @@ __global__ __launch_bounds__(VD_THREADS) void vd_rows_kernel(VerifyArgs a, int c
     } else {
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
-            const int i = 4 * (tid + VD_THREADS * (e / 4)) + e % 4;
+            const int i = 4 * (lane + 64 * (e / 4)) + e % 4;
             x[e] = i < left ? row[i] : -INFINITY;
         }
     }
@@ -121,51 +120,40 @@ __global__ __launch_bounds__(VD_THREADS) void vd_rows_kernel(VerifyArgs a, int c
     for (int e = 0; e < EPT; ++e) { nan |= x[e] != x[e]; m = fmaxf(m, x[e]); }
     m = wave_max(m);
     int arg = 0x7fffffff;
+    if (ARG) {
 #pragma unroll
-    for (int e = EPT - 1; e >= 0; --e)
-        if (x[e] == m) arg = 4 * (tid + VD_THREADS * (e / 4)) + e % 4;
+        for (int e = EPT - 1; e >= 0; --e)
+            if (x[e] == m) arg = 4 * (lane + 64 * (e / 4)) + e % 4;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const int other = __shfl_xor(arg, o, 64);
-        arg = other < arg ? other : arg;
+        for (int o = 32; o > 0; o >>= 1) {
+            const int other = __shfl_xor(arg, o, 64);
+            arg = other < arg ? other : arg;
+        }
     }
     double s = 0.0;
     if (SUMS) {
         const double md = m == -INFINITY ? 0.0 : (double)m, c = 1.4426950408889634074 / (a.temperature > 0 ? a.temperature : 1.0);
+        const double least = -1020.0 / c;
         double s1 = 0.0;
 #pragma unroll
         for (int e = 0; e < EPT; e += 2) {
-            s += vd_exp2(__builtin_fmax(((double)x[e] - md) * c, -1020.0));
-            s1 += vd_exp2(__builtin_fmax(((double)x[e + 1] - md) * c, -1020.0));
+            s += vd_exp(__builtin_fmax((double)x[e] - md, least), c);
+            s1 += vd_exp(__builtin_fmax((double)x[e + 1] - md, least), c);
         }
         s = vd_wave_sum(s + s1);
     }
     nan = __any(nan);
-    if (lane == 0) { s_max[wv] = m; s_arg[wv] = nan ? -1 : arg; s_sum[wv] = s; }
-    __syncthreads();
-    if (tid == 0) {
-        const double c = 1.4426950408889634074 / (a.temperature > 0 ? a.temperature : 1.0);
-        float mm = s_max[0];
-        bool bad = s_arg[0] < 0;
-        int at = s_arg[0];
-        for (int w = 1; w < 4; ++w) {
-            bad |= s_arg[w] < 0;
-            if (s_max[w] > mm || (s_max[w] == mm && s_arg[w] < at)) { mm = s_max[w]; at = s_arg[w]; }
-        }
-        double total = 0.0;
-        if (SUMS)
-            for (int w = 0; w < 4; ++w)
-                if (s_max[w] != -INFINITY) total += s_sum[w] * vd_weight(s_max[w], mm, c);
+    if (lane == 0) {
         VdWs w;
         vd_ws(a.ws, a.B, a.T, chunks, &w);
         const size_t cell = ((size_t)b * (2 * a.T + 1) + r) * chunks + chunk;
-        w.max[cell] = mm;
-        w.arg[cell] = bad ? -1 : (at < left ? at + first : 0x7fffffff);
-        w.sum[cell] = total;
+        w.max[cell] = m;
+        w.arg[cell] = nan ? -1 : (arg < left ? arg + first : 0x7fffffff);
+        w.sum[cell] = s;
     }
 }
 
-// What happens to sequence b, worked out by a whole workgroup (every thread returns it): rows joined from their chunks by a thread
+// What happens to sequence b, worked out by a whole workgroup (every thread returns it): rows joined from their chunks by 16 lanes
 // each, then the first draft that is not accepted.  s_*: shared arrays of 2 T + 1 (T + 1 for s_arg) elements.
 template <int THREADS>
 __device__ VdDecision vd_decide(const VerifyArgs &a, const VdWs &w, int b, int chunks, bool sums, double *s_z, float *s_m, int *s_arg, int *s_stop) {
@@ -174,33 +162,54 @@ __device__ VdDecision vd_decide(const VerifyArgs &a, const VdWs &w, int b, int c
     const double c = 1.4426950408889634074 / (greedy ? 1.0 : a.temperature);
     const int rows = a.draft ? 2 * T + 1 : T + 1;
     if (tid == 0) *s_stop = n;
-    for (int r = tid; r < rows; r += THREADS) {
+    // the first THREADS drafted tokens' logits travel while the rows are joined
+    int x = -1;
+    float xp = 0.f, xq = 0.f, u = 0.f;
+    auto fetch = [&](int i) {
+        x = a.drafts[(size_t)b * T + i];
+        const bool in = x >= 0 && x < a.V;
+        xp = in ? vd_row(a, b, i)[x] : -INFINITY;
+        xq = in && a.draft ? vd_row(a, b, T + 1 + i)[x] : -INFINITY;
+        u = greedy ? 0.f : a.u[(size_t)b * (T + 1) + i];
+    };
+    if (tid < n) fetch(tid);
+    const int l = tid & 15;  // 16 lanes join the chunks of a row
+    for (int r = tid >> 4; r < rows; r += THREADS / 16) {
         if (r <= T ? r > n : r - T - 1 >= n) continue;
         const size_t cell = ((size_t)b * (2 * T + 1) + r) * chunks;
         float m = -INFINITY;
-        int arg = 0x7fffffff;
-        bool bad = false;
-        for (int k = 0; k < chunks; ++k) {
+        int arg = 0x7fffffff, bad = 0;
+#pragma unroll 4
+        for (int k = l; k < chunks; k += 16) {
             const float cm = w.max[cell + k];
             const int ca = w.arg[cell + k];
             bad |= ca < 0;
             if (cm > m || (cm == m && ca < arg)) { m = cm; arg = ca; }
         }
-        if (!greedy && !(fabsf(m) < INFINITY)) bad = true;
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) {
+            const float om = __shfl_xor(m, o, 64);
+            const int oa = __shfl_xor(arg, o, 64);
+            bad |= __shfl_xor(bad, o, 64);
+            if (om > m || (om == m && oa < arg)) { m = om; arg = oa; }
+        }
+        const bool finite = fabsf(m) < INFINITY;
         double z = 0.0;
-        if (sums && !bad && fabsf(m) < INFINITY)
-            for (int k = 0; k < chunks; ++k) {
+        if (sums && finite) {
+#pragma unroll 4
+            for (int k = l; k < chunks; k += 16) {
                 const float cm = w.max[cell + k];
-                if (cm != -INFINITY) z += w.sum[cell + k] * vd_weight(cm, m, c);
+                z += cm == -INFINITY ? 0.0 : w.sum[cell + k] * vd_weight(cm, m, c);
             }
-        s_m[r] = m;
-        s_z[r] = z;
-        s_arg[r] = bad ? -1 : arg;
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) z += __shfl_xor(z, o, 64);
+        }
+        if (l == 0) { s_m[r] = m; s_z[r] = z; s_arg[r] = bad || (!greedy && !finite) ? -1 : arg; }
     }
     __syncthreads();
     for (int i = tid; i < n; i += THREADS) {
+        if (i != tid) fetch(i);
         bool go = s_arg[i] >= 0;
-        const int x = a.drafts[(size_t)b * T + i];
         if (greedy) {
             go = go && x == s_arg[i];
         } else if (go) {
@@ -209,9 +218,9 @@ __device__ VdDecision vd_decide(const VerifyArgs &a, const VdWs &w, int b, int c
             if (a.draft) {
                 const int r = T + 1 + i;
                 go = s_arg[r] >= 0;
-                if (go && in) q = vd_weight(vd_row(a, b, r)[x], s_m[r], c) / s_z[r];
+                if (go) q = vd_weight(xq, s_m[r], c) / s_z[r];
             }
-            go = go && in && (double)a.u[(size_t)b * (T + 1) + i] * q < vd_weight(vd_row(a, b, i)[x], s_m[i], c) / s_z[i];
+            go = go && in && (double)u * q < vd_weight(xp, s_m[i], c) / s_z[i];
         }
         if (!go) atomicMin(s_stop, i);
     }
@@ -226,17 +235,17 @@ __device__ VdDecision vd_decide(const VerifyArgs &a, const VdWs &w, int b, int c
 
 #define VD_MAX_ROWS (2 * 256 + 1)
 
-// Weights max(0, p - q) of the rejected position, summed per chunk: one workgroup per (sequence, chunk).  The decision is worked out in
-// each (a launch of its own would cost more); the first chunk's workgroup keeps it for the choice.
-__global__ __launch_bounds__(VD_THREADS) void vd_residual_kernel(VerifyArgs a, int chunks, int chunk_len) {
-    __shared__ double s_z[VD_MAX_ROWS], s_sum[4];
+// Weights max(0, p - q) of the rejected position, summed per chunk: a wavefront per chunk, four chunks per workgroup.  The decision is
+// worked out in each workgroup (a launch of its own would cost more); the first of a sequence keeps it for the choice.
+__global__ __launch_bounds__(VD_THREADS) void vd_residual_kernel(VerifyArgs a, int chunks, int chunk_len, int groups) {
+    __shared__ double s_z[VD_MAX_ROWS];
     __shared__ float s_m[VD_MAX_ROWS];
     __shared__ int s_arg[VD_MAX_ROWS], s_stop;
-    const int chunk = blockIdx.x % chunks, b = blockIdx.x / chunks, tid = threadIdx.x;
+    const int group = blockIdx.x % groups, b = blockIdx.x / groups, tid = threadIdx.x, lane = tid & 63, chunk = group * 4 + (tid >> 6);
     VdWs w;
     vd_ws(a.ws, a.B, a.T, chunks, &w);
     const VdDecision d = vd_decide<VD_THREADS>(a, w, b, chunks, true, s_z, s_m, s_arg, &s_stop);
-    if (chunk == 0) {
+    if (group == 0) {
         if (tid == 0) w.dec[b] = d;
         const int rows = 2 * a.T + 1;
         for (int r = tid; r < rows; r += VD_THREADS)
@@ -245,28 +254,35 @@ __global__ __launch_bounds__(VD_THREADS) void vd_residual_kernel(VerifyArgs a, i
                 w.row_sum[(size_t)b * rows + r] = s_z[r];
             }
     }
-    if (d.bad || !d.rejected) return;
+    if (d.bad || !d.rejected || chunk >= chunks) return;
     const int rp = d.stop, rq = a.T + 1 + d.stop;
     const double c = 1.4426950408889634074 / a.temperature, mp = s_m[rp], mq = s_m[rq], ip = 1.0 / s_z[rp], iq = 1.0 / s_z[rq];
     const float *prow = vd_row(a, b, rp), *qrow = vd_row(a, b, rq);
     const int first = chunk * chunk_len, last = first + chunk_len < a.V ? first + chunk_len : a.V;
     double s = 0.0;
-#pragma unroll 4
-    for (int v = first + tid; v < last; v += VD_THREADS) {
-        const double e = vd_weight(prow[v], mp, c) * ip - vd_weight(qrow[v], mq, c) * iq;
+    auto add = [&](float x, float y) {
+        const double e = vd_weight(x, mp, c) * ip - vd_weight(y, mq, c) * iq;
         s += e > 0.0 ? e : 0.0;
+    };
+    const bool whole = ((reinterpret_cast<uintptr_t>(prow + first) | reinterpret_cast<uintptr_t>(qrow + first)) & 15) == 0;
+    const int vectors = whole ? (last - first) / 4 : 0;
+#pragma unroll 4
+    for (int i = lane; i < vectors; i += 64) {
+        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(prow + first + 4 * i), y = *reinterpret_cast<const f32x4_t *>(qrow + first + 4 * i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) add(x[e], y[e]);
     }
+#pragma unroll 4
+    for (int v = first + 4 * vectors + lane; v < last; v += 64) add(prow[v], qrow[v]);
     s = vd_wave_sum(s);
-    if ((tid & 63) == 0) s_sum[tid >> 6] = s;
-    __syncthreads();
-    if (tid == 0) w.mass[(size_t)b * chunks + chunk] = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
+    if (lane == 0) w.mass[(size_t)b * chunks + chunk] = s;
 }
 
 // The next token and the outputs: one workgroup per sequence.  DECIDE: no residual kernel ran (greedy, or drafts that were not
 // sampled), so the decision is worked out here.
-template <bool DECIDE>
-__global__ __launch_bounds__(VD_PICK_THREADS) void vd_pick_kernel(VerifyArgs a, int chunks, int chunk_len) {
-    constexpr int WAVES = VD_PICK_THREADS / RL_WAVE;
+template <bool DECIDE, int PER>
+__global__ __launch_bounds__(VD_PICK_THREADS) void vd_pick_kernel(VerifyArgs a, int chunks) {
+    constexpr int WAVES = VD_PICK_THREADS / RL_WAVE, chunk_len = VD_PICK_THREADS * PER;
     __shared__ double s_z[VD_MAX_ROWS], s_red[WAVES], s_before, s_total, s_part;
     __shared__ float s_m[VD_MAX_ROWS];
     __shared__ int s_arg[VD_MAX_ROWS], s_stop, s_chunk, s_owner, s_next;
@@ -298,11 +314,11 @@ __global__ __launch_bounds__(VD_PICK_THREADS) void vd_pick_kernel(VerifyArgs a, 
         const float *qrow = sampled ? vd_row(a, b, rq) : nullptr;
         const double mq = sampled ? (double)s_m[rq] : 0.0, iq = sampled ? 1.0 / s_z[rq] : 0.0;
         bool residual = d.rejected;
-        auto weight = [&](int v) -> double {
-            const double p = vd_weight(prow[v], mp, c) * ip;
+        auto weight_of = [&](int v, float xp, float xq) -> double {
+            const double p = vd_weight(xp, mp, c) * ip;
             if (!residual) return p;
             if (!sampled) return v == d.token ? 0.0 : p;
-            const double e = p - vd_weight(qrow[v], mq, c) * iq;
+            const double e = p - vd_weight(xq, mq, c) * iq;
             return e > 0.0 ? e : 0.0;
         };
         // a drafted token that was not sampled leaves its own chunk without its weight: that chunk is summed again
@@ -310,7 +326,11 @@ __global__ __launch_bounds__(VD_PICK_THREADS) void vd_pick_kernel(VerifyArgs a, 
         if (own >= 0) {
             const int last = (own + 1) * chunk_len < a.V ? (own + 1) * chunk_len : a.V;
             double s = 0.0;
-            for (int v = own * chunk_len + tid; v < last; v += VD_PICK_THREADS) s += weight(v);
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                const int v = own * chunk_len + tid + k * VD_PICK_THREADS;
+                s += v < last ? weight_of(v, prow[v], 0.f) : 0.0;
+            }
             s = vd_wave_sum(s);
             if (lane == 0) s_red[wv] = s;
             __syncthreads();
@@ -380,10 +400,20 @@ __global__ __launch_bounds__(VD_PICK_THREADS) void vd_pick_kernel(VerifyArgs a, 
         // within the chunk: every thread owns consecutive tokens, their sums are scanned in order, the first thread whose running sum
         // exceeds the draw walks its own
         const int first = s_chunk * chunk_len, last = first + chunk_len < a.V ? first + chunk_len : a.V;
-        const int per = (chunk_len + VD_PICK_THREADS - 1) / VD_PICK_THREADS;
-        const int i0 = first + tid * per < last ? first + tid * per : last, i1 = i0 + per < last ? i0 + per : last;
-        double s = 0.0;
-        for (int v = i0; v < i1; ++v) s += weight(v);
+        const int i0 = first + tid * PER;
+        float xp[PER], xq[PER];
+        double e[PER], s = 0.0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int v = i0 + k < last ? i0 + k : last - 1;  // loads without conditions: all of them in flight
+            xp[k] = prow[v];
+            xq[k] = residual && sampled ? qrow[v] : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            e[k] = i0 + k < last ? weight_of(i0 + k, xp[k], xq[k]) : 0.0;
+            s += e[k];
+        }
         double incl = s;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -398,18 +428,21 @@ __global__ __launch_bounds__(VD_PICK_THREADS) void vd_pick_kernel(VerifyArgs a, 
         __syncthreads();
         if (tid == s_owner) {
             double run = before + incl - s;
-            int pick = i0;
-            for (int v = i0; v < i1; ++v) {
-                const double e = weight(v);
-                if (e > 0.0) pick = v;
-                run += e;
-                if (e > 0.0 && run > target) break;
+            int pick = -1, last_pick = i0;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                run += e[k];
+                if (e[k] > 0.0) {
+                    last_pick = i0 + k;
+                    if (pick < 0 && run > target) pick = i0 + k;
+                }
             }
-            s_next = pick;
+            s_next = pick >= 0 ? pick : last_pick;
         } else if (s_owner == VD_PICK_THREADS && s > 0.0) {  // by rounding nobody's: the last token with weight
             int pick = i0;
-            for (int v = i0; v < i1; ++v)
-                if (weight(v) > 0.0) pick = v;
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+                if (e[k] > 0.0) pick = i0 + k;
             atomicMax(&s_next, pick);
         }
         __syncthreads();
@@ -425,27 +458,29 @@ __global__ __launch_bounds__(VD_PICK_THREADS) void vd_pick_kernel(VerifyArgs a, 
     }
 }
 
-// Logits per workgroup: 8192 where that still gives every compute unit a few workgroups, else 2048.
-static int vd_per_thread(int B, int T, int V) { return (int64_t)B * (T + 1) * ceil_div(V, 8192) >= 512 ? 32 : 8; }
+// Logits per wavefront: 2048 where that still gives every compute unit a dozen wavefronts, else 512.
+static int vd_chunk_len(int B, int T, int V) { return (int64_t)B * (T + 1) * ceil_div(V, 2048) >= 2048 ? 2048 : 512; }
 
-size_t verify_drafts_ws_bytes(int B, int T, int V) {
-    return vd_ws(nullptr, B, T, ceil_div(V, VD_THREADS * vd_per_thread(B, T, V)), nullptr) + 8;
+size_t verify_drafts_ws_bytes(int B, int T, int V) { return vd_ws(nullptr, B, T, ceil_div(V, vd_chunk_len(B, T, V)), nullptr) + 8; }
+
+template <int EPT>
+static void vd_launch(const VerifyArgs &a, hipStream_t st) {
+    constexpr int LEN = 64 * EPT, PER = LEN / VD_PICK_THREADS;
+    const int chunks = ceil_div(a.V, LEN), rows = a.draft ? 2 * a.T + 1 : a.T + 1, groups = ceil_div(chunks, 4);
+    const unsigned blocks = (unsigned)((int64_t)a.B * rows * groups);
+    if (a.temperature > 0) vd_rows_kernel<EPT, true, false><<<blocks, VD_THREADS, 0, st>>>(a, chunks, rows, groups);
+    else if (a.logp) vd_rows_kernel<EPT, true, true><<<blocks, VD_THREADS, 0, st>>>(a, chunks, rows, groups);
+    else vd_rows_kernel<EPT, false, true><<<blocks, VD_THREADS, 0, st>>>(a, chunks, rows, groups);
+    if (a.draft) {
+        vd_residual_kernel<<<a.B * groups, VD_THREADS, 0, st>>>(a, chunks, LEN, groups);
+        vd_pick_kernel<false, PER><<<a.B, VD_PICK_THREADS, 0, st>>>(a, chunks);
+    } else {
+        vd_pick_kernel<true, PER><<<a.B, VD_PICK_THREADS, 0, st>>>(a, chunks);
+    }
 }
 
 void launch_verify_drafts(const VerifyArgs &a, hipStream_t st) {
     if (a.B <= 0) return;
-    const int ept = vd_per_thread(a.B, a.T, a.V), chunk_len = VD_THREADS * ept, chunks = ceil_div(a.V, chunk_len);
-    const int rows = a.draft ? 2 * a.T + 1 : a.T + 1;
-    const unsigned blocks = (unsigned)((int64_t)a.B * rows * chunks);
-    const bool sums = a.temperature > 0 || a.logp;
-    if (ept == 32 && sums) vd_rows_kernel<32, true><<<blocks, VD_THREADS, 0, st>>>(a, chunks, rows);
-    else if (ept == 32) vd_rows_kernel<32, false><<<blocks, VD_THREADS, 0, st>>>(a, chunks, rows);
-    else if (sums) vd_rows_kernel<8, true><<<blocks, VD_THREADS, 0, st>>>(a, chunks, rows);
-    else vd_rows_kernel<8, false><<<blocks, VD_THREADS, 0, st>>>(a, chunks, rows);
-    if (a.draft) {
-        vd_residual_kernel<<<a.B * chunks, VD_THREADS, 0, st>>>(a, chunks, chunk_len);
-        vd_pick_kernel<false><<<a.B, VD_PICK_THREADS, 0, st>>>(a, chunks, chunk_len);
-    } else {
-        vd_pick_kernel<true><<<a.B, VD_PICK_THREADS, 0, st>>>(a, chunks, chunk_len);
-    }
+    if (vd_chunk_len(a.B, a.T, a.V) == 2048) vd_launch<32>(a, st);
+    else vd_launch<8>(a, st);
 }
