@@ -3,10 +3,12 @@
 // The T tokens of a sequence and the G = Hq / Hkv query heads of a kv head are R = T * G query rows that share every cache row: per tile
 // of 32 cache rows two matrix products,
 //     S^T[32 keys x 16 columns] = K[32 x hd] * Q^T[hd x 16],     O^T[hd x 16 columns] += V^T[hd x 32 keys] * P^T[32 x 16],
-// where 16 columns are the high and the low half term of 8 query rows (columns c and c + 8): q and the probabilities enter the
-// matrix cores with about 22 significant bits, K and V as stored (a block-scaled int16 n as the exact sum of the two halves
-// n & ~31 and n & 31).  A wavefront takes NT = 1, 2 or 4 such column tiles (8, 16 or 32 query rows); more rows are further workgroups
-// that find the cache rows in the L2 of their XCD.  S^T leaves a lane with 4 keys of a column per 16-key product, which is the
+// where q and the probabilities enter the matrix cores as two half terms, with about 22 significant bits, and K and V as stored.  Up to 8
+// query rows share the 16 columns with their low terms (columns c and c + 8: one product for both); with more a column is a row
+// and the low terms take a second product, which leaves the softmax without idle lanes (32 rows of the 32/8-head case: 77 -> XX us).
+// A wavefront takes 8, 16 or 32 query rows; more rows are further workgroups that find the cache rows in the L2 of their XCD.
+// A block-scaled int16 n = 64 h + l is taken as h + l / 64: two exact halves by packed 16-bit instructions, five for two elements (h in
+// [-512, 511] and l / 64 in [0, 1) come out of the mantissa of 1024 + x and 16 + x / 64), the factor 64 goes with the row scale.  S^T leaves a lane with 4 keys of a column per 16-key product, which is the
 // layout that P^T needs: key 4 j + i of the first 16 keys is contraction index 8 j + i, of the second 8 j + 4 + i.
 //
 // One pass with a running maximum and sum per query row.  The maximum is raised (and the accumulators rescaled) only when a score
@@ -35,6 +37,15 @@ __device__ __forceinline__ float span_max_groups(float v) {  // over the four la
     return fmaxf(v, __shfl_xor(v, 32, 64));
 }
 
+// Eight int16 elements n = 64 h + l as h and l / 64.
+__device__ __forceinline__ void span_split(u32x4_t n, f16x8_t *h, f16x8_t *l) {
+    typedef uint16_t u16x8_t __attribute__((ext_vector_type(8)));
+    const u16x8_t top = (__builtin_bit_cast(u16x8_t, n) >> (uint16_t)6) ^ (uint16_t)0x6600;  // 1024 + (h + 512) as a half
+    const u32x4_t low = (n & 0x003f003fu) | 0x4c004c00u;                                    // 16 + l / 64
+    *h = __builtin_bit_cast(f16x8_t, top) - (_Float16)1536.f;
+    *l = __builtin_bit_cast(f16x8_t, low) - (_Float16)16.f;
+}
+
 // Rows of the workspace: statistics (max, sum) of every (query row, split), then partial outputs (nsplit > 1), then scores (weights).
 struct SpanWs {
     size_t stats, part, scores, total;  // offsets in floats
@@ -60,7 +71,8 @@ __device__ __forceinline__ void span_extent(const SpanArgs &a, int b, int *n0, i
 }
 
 // ONCE: no other workgroup reads these cache rows (one row tile), so their copies are non-temporal: they stream faster.
-template <int HD, int NT, int W, bool I16, bool ONCE>
+// RT: 0: 8 query rows with both terms in one tile; 1, 2: so many tiles of 16 rows.
+template <int HD, int RT, int W, bool I16, bool ONCE>
 __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int row_tiles, int items) {
     constexpr int RB = HD * 2;                    // bytes of a cache row
     constexpr int KS = HD / 32, OT = HD / 16;     // k-steps of a score, tiles of the output
@@ -68,7 +80,7 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
     constexpr int STAGE = 2 * TILEB + (I16 ? 512 : 0);
     constexpr int NST = HD == 128 ? 2 : 4;        // 32 KB of ring per wavefront: five of them, or one workgroup of four, per compute unit
     constexpr int LPR = RB / 16;                  // lanes per row of a copy instruction
-    constexpr int ROWS = 8 * NT;                  // query rows of this workgroup
+    constexpr int NT = RT ? RT : 1, TR = RT ? 16 : 8, ROWS = TR * NT;  // column tiles, query rows of a tile and of this workgroup
     __shared__ __attribute__((aligned(1024))) unsigned char ring_all[W * NST * STAGE];
     static_assert(ROWS * (HD + 2) * 4 <= NST * STAGE, "the join reuses the ring");
 
@@ -100,13 +112,13 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
     const int j1 = __builtin_amdgcn_readfirstlane(nmax - j0 > chunk ? j0 + chunk : nmax);
     const int ntiles = (j1 - j0 + kSpanTile - 1) / kSpanTile;
 
-    // ---- Q^T operands: column c of tile nt = query row r0 + 8 nt + (c & 7), term c >> 3; k-step s covers elements 32 s + 8 j + 0..7
-    f16x8_t qf[NT][KS];
+    // ---- Q^T operands: column c of tile nt = query row r0 + TR nt + c % TR; k-step s covers elements 32 s + 8 j + 0..7
+    f16x8_t qf[NT][KS], ql[RT ? NT : 1][RT ? KS : 1];
     int lim[NT];
     const float qscale = rsqrtf((float)HD) * 1.44269504f;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        const int rr = r0 + 8 * nt + (c & 7);
+        const int rr = r0 + TR * nt + c % TR;
         const bool ok = rr <= rlast;
         const int rc = ok ? rr : rlast;
         lim[nt] = limit(rc);
@@ -119,7 +131,8 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
                 const float v = ok ? (e < 4 ? x0[e & 3] : x1[e & 3]) * qscale : 0.f;
                 const _Float16 hi = (_Float16)__builtin_amdgcn_fmed3f(v, -65504.f, 65504.f);  // saturating, like every half here
                 const _Float16 lo = (_Float16)__builtin_amdgcn_fmed3f(v - (float)hi, -65504.f, 65504.f);
-                qf[nt][s][e] = c < 8 ? hi : lo;
+                qf[nt][s][e] = RT || c < 8 ? hi : lo;
+                if (RT) ql[RT ? nt : 0][RT ? s : 0][e] = lo;
             }
         }
     }
@@ -227,20 +240,15 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 const u32x4_t kw = *reinterpret_cast<const u32x4_t *>(st + h * 16 * RB + kaddr[s]);
-                if (I16) {
-                    const u32x4_t wh = {kw.x & 0xFFE0FFE0u, kw.y & 0xFFE0FFE0u, kw.z & 0xFFE0FFE0u, kw.w & 0xFFE0FFE0u};
-                    const u32x4_t wl = {kw.x & 0x001F001Fu, kw.y & 0x001F001Fu, kw.z & 0x001F001Fu, kw.w & 0x001F001Fu};
-                    const f16x8_t kh = __builtin_convertvector(__builtin_bit_cast(s16x8_t, wh), f16x8_t);
-                    const f16x8_t kl = __builtin_convertvector(__builtin_bit_cast(s16x8_t, wl), f16x8_t);
+                f16x8_t kh, kl;
+                if (I16) span_split(kw, &kh, &kl);
+                else kh = __builtin_bit_cast(f16x8_t, kw);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        sacc[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qf[nt][s], sacc[nt][h], 0, 0, 0);
-                        sacc[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, qf[nt][s], sacc[nt][h], 0, 0, 0);
-                    }
-                } else {
-                    const f16x8_t kf = __builtin_bit_cast(f16x8_t, kw);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) sacc[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[nt][s], sacc[nt][h], 0, 0, 0);
+                for (int nt = 0; nt < NT; ++nt) {
+                    sacc[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qf[nt][s], sacc[nt][h], 0, 0, 0);
+                    if (RT) sacc[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, ql[RT ? nt : 0][RT ? s : 0], sacc[nt][h], 0, 0, 0);
+                    if (I16) sacc[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, qf[nt][s], sacc[nt][h], 0, 0, 0);
+                    if (I16 && RT) sacc[nt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, ql[RT ? nt : 0][RT ? s : 0], sacc[nt][h], 0, 0, 0);
                 }
             }
         f32x4_t ksc[2], vsc[2];
@@ -274,7 +282,7 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
                             if ((v & 0x7c00u) == 0x7c00u) {
 #pragma unroll
                                 for (int nt = 0; nt < NT; ++nt)
-                                    if (c < 8 && key0 + k < lim[nt]) acc[nt][t][i] += f16_to_f32(v);
+                                    if ((RT || c < 8) && key0 + k < lim[nt]) acc[nt][t][i] += f16_to_f32(v);
                             }
                         }
                 __builtin_amdgcn_wave_barrier();
@@ -292,15 +300,15 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
                 __builtin_amdgcn_wave_barrier();
             }
         }
-        f16x8_t pf[NT];
+        f16x8_t pf[NT], pl[RT ? NT : 1];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float x = sacc[nt][e >> 2][e & 3];
-                x += span_ror8(x);                // high and low term of the query row
-                if (I16) x *= ksc[e >> 2][e & 3];
+                if (!RT) x += span_ror8(x);       // high and low term of the query row
+                if (I16) x *= ksc[e >> 2][e & 3] * 64.f;
                 v[e] = x;
             }
             if (tail) {
@@ -308,8 +316,8 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
                 for (int e = 0; e < 8; ++e)
                     if (key0 + 16 * (e >> 2) + 4 * j + (e & 3) >= (lim[nt] < j1 ? lim[nt] : j1)) v[e] = -INFINITY;
             }
-            if (a.weight && c < 8 && r0 + 8 * nt + c <= rlast) {
-                float *sp = scores + (size_t)(r0 + 8 * nt + c) * w.ld + key0 + 4 * j;
+            if (a.weight && (RT || c < 8) && r0 + TR * nt + c <= rlast) {
+                float *sp = scores + (size_t)(r0 + TR * nt + c) * w.ld + key0 + 4 * j;
                 *reinterpret_cast<f32x4_t *>(sp) = f32x4_t{v[0], v[1], v[2], v[3]};
                 *reinterpret_cast<f32x4_t *>(sp + 16) = f32x4_t{v[4], v[5], v[6], v[7]};
             }
@@ -353,10 +361,13 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
                 inv = ref[nt] > 0.f ? __builtin_amdgcn_rcpf(ref[nt]) : 0.f;
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float x = I16 ? v[e] * inv : v[e];
-                const _Float16 hi = (_Float16)x;
-                pf[nt][e] = c < 8 ? hi : (_Float16)(x - (float)hi);
+            for (int e = 0; e < 8; e += 2) {      // the high term cut off, the low term takes what is left
+                const float x0 = I16 ? v[e] * inv : v[e], x1 = I16 ? v[e + 1] * inv : v[e + 1];
+                const f16x2_t hi = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_pkrtz(x0, x1));
+                const f16x2_t lo = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_pkrtz(x0 - (float)hi.x, x1 - (float)hi.y));
+                pf[nt][e] = RT || c < 8 ? hi.x : lo.x;
+                pf[nt][e + 1] = RT || c < 8 ? hi.y : lo.y;
+                if (RT) { pl[RT ? nt : 0][e] = lo.x; pl[RT ? nt : 0][e + 1] = lo.y; }
             }
         }
         s16x4_t vt[OT][2];
@@ -380,17 +391,15 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
 #pragma unroll
         for (int t = 0; t < OT; ++t) {
             const s16x8_t vw = __builtin_shufflevector(vt[t][0], vt[t][1], 0, 1, 2, 3, 4, 5, 6, 7);
-            if (I16) {
-                const f16x8_t vh = __builtin_convertvector(vw & (short)0xFFE0, f16x8_t), vl = __builtin_convertvector(vw & (short)0x001F, f16x8_t);
+            f16x8_t vh, vl;
+            if (I16) span_split(__builtin_bit_cast(u32x4_t, vw), &vh, &vl);
+            else vh = __builtin_bit_cast(f16x8_t, vw);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, pf[nt], acc[nt][t], 0, 0, 0);
-                    acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, pf[nt], acc[nt][t], 0, 0, 0);
-                }
-            } else {
-                const f16x8_t vf = __builtin_bit_cast(f16x8_t, vw);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[nt], acc[nt][t], 0, 0, 0);
+            for (int nt = 0; nt < NT; ++nt) {
+                acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, pf[nt], acc[nt][t], 0, 0, 0);
+                if (RT) acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, pl[RT ? nt : 0], acc[nt][t], 0, 0, 0);
+                if (I16) acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, pf[nt], acc[nt][t], 0, 0, 0);
+                if (I16 && RT) acc[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, pl[RT ? nt : 0], acc[nt][t], 0, 0, 0);
             }
         }
     };
@@ -426,14 +435,14 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
         float d = den[nt];
         d += __shfl_xor(d, 16, 64);
         d += __shfl_xor(d, 32, 64);
-        if (j == 0 && c < 8) { s_max(wave, 8 * nt + c) = mrun[nt]; s_den(wave, 8 * nt + c) = d; }
+        if (j == 0 && c < TR) { s_max(wave, TR * nt + c) = mrun[nt]; s_den(wave, TR * nt + c) = d; }
 #pragma unroll
         for (int t = 0; t < OT; ++t) {
             f32x4_t o;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = acc[nt][t][i] + span_ror8(acc[nt][t][i]);
-            if (I16) o = o * ref[nt];
-            if (c < 8) *reinterpret_cast<f32x4_t *>(part + (8 * nt + c) * HD + 16 * t + 4 * j) = o;
+            for (int i = 0; i < 4; ++i) o[i] = RT ? acc[nt][t][i] : acc[nt][t][i] + span_ror8(acc[nt][t][i]);
+            if (I16) o = o * (ref[nt] * 64.f);
+            if (c < TR) *reinterpret_cast<f32x4_t *>(part + (TR * nt + c) * HD + 16 * t + 4 * j) = o;
         }
     }
     __syncthreads();
@@ -562,13 +571,13 @@ __global__ __launch_bounds__(256) void span_join_kernel(SpanArgs a, int merge_bl
         if (key + i < n) wt[i] += sum[i];
 }
 
-// Query rows of a workgroup: as many column tiles as the rows fill, up to four.
-static int span_tiles(int T, int G) {
-    const int R = T * G;
-    return R <= 8 ? 1 : R <= 16 ? 2 : 4;
+// Query rows of a workgroup.
+static int span_rows(int T, int G) {
+    const int64_t R = (int64_t)T * G;
+    return R <= 8 ? 8 : R <= 16 ? 16 : 32;
 }
 static int64_t span_items(int B, int T, int Hq, int Hkv) {
-    const int G = Hq / Hkv, rows = 8 * span_tiles(T, G);
+    const int G = Hq / Hkv, rows = span_rows(T, G);
     return (int64_t)B * Hkv * ((T * (int64_t)G + rows - 1) / rows);
 }
 
@@ -585,24 +594,23 @@ size_t span_attention_ws_floats(int B, int T, int Hq, int Hkv, int hd, int S, in
     return span_ws(B, T, Hq, hd, S, nsplit, weights).total;
 }
 
-template <int HD, int NT, bool I16, bool ONCE>
+template <int HD, int RT, bool I16, bool ONCE>
 static void span_launch(const SpanArgs &a, int row_tiles, hipStream_t st) {
     const int items = a.B * a.Hkv * a.nsplit;
     const unsigned blocks = (unsigned)((int64_t)ceil_div(items, 8) * 8 * row_tiles);
     // wavefronts that share a sequence's rows: enough of them for the compute units when there are few items
     const int64_t work = (int64_t)items * row_tiles;
-    if (work <= 256) span_attention_kernel<HD, NT, 4, I16, ONCE><<<blocks, 256, 0, st>>>(a, row_tiles, items);
-    else if (work <= 512) span_attention_kernel<HD, NT, 2, I16, ONCE><<<blocks, 128, 0, st>>>(a, row_tiles, items);
-    else span_attention_kernel<HD, NT, 1, I16, ONCE><<<blocks, 64, 0, st>>>(a, row_tiles, items);
+    if (work <= 256) span_attention_kernel<HD, RT, 4, I16, ONCE><<<blocks, 256, 0, st>>>(a, row_tiles, items);
+    else if (work <= 512) span_attention_kernel<HD, RT, 2, I16, ONCE><<<blocks, 128, 0, st>>>(a, row_tiles, items);
+    else span_attention_kernel<HD, RT, 1, I16, ONCE><<<blocks, 64, 0, st>>>(a, row_tiles, items);
 }
 template <int HD, bool I16>
 static void span_launch_tiles(const SpanArgs &a, hipStream_t st) {
-    const int G = a.Hq / a.Hkv, nt = span_tiles(a.T, G);
-    const int row_tiles = (int)((a.T * (int64_t)G + 8 * nt - 1) / (8 * nt));
-    if (nt == 1) span_launch<HD, 1, I16, true>(a, 1, st);
-    else if (nt == 2) span_launch<HD, 2, I16, true>(a, 1, st);
-    else if (row_tiles == 1) span_launch<HD, 4, I16, true>(a, 1, st);
-    else span_launch<HD, 4, I16, false>(a, row_tiles, st);
+    const int G = a.Hq / a.Hkv, rows = span_rows(a.T, G), row_tiles = (int)((a.T * (int64_t)G + rows - 1) / rows);
+    if (rows == 8) span_launch<HD, 0, I16, true>(a, 1, st);
+    else if (rows == 16) span_launch<HD, 1, I16, true>(a, 1, st);
+    else if (row_tiles == 1) span_launch<HD, 2, I16, true>(a, 1, st);
+    else span_launch<HD, 2, I16, false>(a, row_tiles, st);
 }
 
 void launch_span_attention(const SpanArgs &a, hipStream_t st) {
