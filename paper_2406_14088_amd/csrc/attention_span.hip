@@ -22,6 +22,8 @@
 // kernel, which also turns the scores kept in the workspace into weights.
 #include "kernels.h"
 
+#include <type_traits>
+
 #define SPAN_LDS(p) ((__attribute__((address_space(3))) void *)(p))
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -46,19 +48,29 @@ __device__ __forceinline__ void span_split(u32x4_t n, f16x8_t *h, f16x8_t *l) {
     *l = __builtin_bit_cast(f16x8_t, low) - (_Float16)16.f;
 }
 
-// Rows of the workspace: statistics (max, sum) of every (query row, split), then partial outputs (nsplit > 1), then scores (weights).
+// Query rows of a workgroup.
+__host__ __device__ static inline int span_rows(int T, int G) {
+    const int64_t R = (int64_t)T * G;
+    return R <= 8 ? 8 : R <= 16 ? 16 : 32;
+}
+
+// The workspace: statistics (max, sum) of every (query row, split), then partial outputs (nsplit > 1), then scores (weights) -- of every
+// (sequence, kv head, workgroup's query rows, tile of cache rows) a block of [query rows][32], written as whole lines.
 struct SpanWs {
     size_t stats, part, scores, total;  // offsets in floats
-    int ld;                             // floats per row of scores
+    size_t slab;                        // floats of scores per (sequence, kv head)
+    int tiles;                          // blocks of a workgroup's query rows
 };
-__host__ __device__ static inline SpanWs span_ws(int B, int T, int Hq, int hd, int S, int nsplit, bool weights) {
+__host__ __device__ static inline SpanWs span_ws(int B, int T, int Hq, int Hkv, int hd, int S, int nsplit, bool weights) {
     SpanWs w;
     const size_t rows = (size_t)B * T * Hq;
-    w.ld = (S + kSpanTile - 1) / kSpanTile * kSpanTile;
+    const int G = Hq / Hkv, per = span_rows(T, G);
+    w.tiles = (S + kSpanTile - 1) / kSpanTile;
+    w.slab = (size_t)((T * (int64_t)G + per - 1) / per) * per * w.tiles * kSpanTile;
     w.stats = 0;
     w.part = nsplit > 1 || weights ? (rows * nsplit * 2 + 3) / 4 * 4 : 0;
     w.scores = w.part + (nsplit > 1 ? rows * nsplit * hd : 0);
-    w.total = w.scores + (weights ? rows * w.ld : 0);
+    w.total = w.scores + (weights ? (size_t)B * Hkv * w.slab : 0);
     return w;
 }
 
@@ -72,17 +84,18 @@ __device__ __forceinline__ void span_extent(const SpanArgs &a, int b, int *n0, i
 
 // ONCE: no other workgroup reads these cache rows (one row tile), so their copies are non-temporal: they stream faster.
 // RT: 0: 8 query rows with both terms in one tile; 1, 2: so many tiles of 16 rows.
-template <int HD, int RT, int W, bool I16, bool ONCE>
-__global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int row_tiles, int items) {
+// WT: the scores are kept and the weights added up.
+template <int HD, int RT, int W, bool I16, bool ONCE, bool WT>
+__global__ __launch_bounds__(64 * W, 2) void span_attention_kernel(SpanArgs a, int row_tiles, int items) {
     constexpr int RB = HD * 2;                    // bytes of a cache row
     constexpr int KS = HD / 32, OT = HD / 16;     // k-steps of a score, tiles of the output
     constexpr int TILEB = kSpanTile * RB;
-    constexpr int STAGE = 2 * TILEB + (I16 ? 512 : 0);
-    constexpr int NST = HD == 128 ? 2 : 4;        // 32 KB of ring per wavefront: five of them, or one workgroup of four, per compute unit
+    constexpr int STAGE = TILEB + (I16 ? 512 : 0);  // a V tile and the row scales of K and V
     constexpr int LPR = RB / 16;                  // lanes per row of a copy instruction
     constexpr int NT = RT ? RT : 1, TR = RT ? 16 : 8, ROWS = TR * NT;  // column tiles, query rows of a tile and of this workgroup
-    __shared__ __attribute__((aligned(1024))) unsigned char ring_all[W * NST * STAGE];
-    static_assert(ROWS * (HD + 2) * 4 <= NST * STAGE, "the join reuses the ring");
+    constexpr int OWN = 2 * STAGE > ROWS * (HD + 2) * 4 ? 2 * STAGE : (ROWS * (HD + 2) * 4 + 1023) / 1024 * 1024;  // LDS of a wavefront
+    __shared__ __attribute__((aligned(1024))) unsigned char ring_all[W * OWN];
+    __shared__ float s_rows[2][ROWS];             // of every query row: maximum, 1 / sum
 
     // Row tiles of one item run at the same time on the same XCD (workgroups that are congruent modulo 8 share one).
     const int bid = blockIdx.x, rem = bid % (8 * row_tiles);
@@ -104,48 +117,51 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
 
     const int wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int c = lane & 15, j = lane >> 4;       // column / group of 4 keys
-    unsigned char *ring = ring_all + wave * (NST * STAGE);
+    unsigned char *ring = ring_all + wave * (OWN);
+    // Rows of a split: the same for all sequences, from the longest of them, so that workgroups have equal work whatever the lengths
+    // (a short sequence has no rows in its last splits).
+    int longest = nmax;
+    if (a.nsplit > 1) {
+        for (int i = lane; i < a.B; i += 64) longest = a.d_len[i] > longest ? a.d_len[i] : longest;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            const int x = __shfl_xor(longest, o, 64);
+            longest = x > longest ? x : longest;
+        }
+        longest = __builtin_amdgcn_readfirstlane(longest < a.S - a.T ? longest + a.T : a.S);
+    }
     const int parts = a.nsplit * W;
-    const int chunk = ((nmax + parts - 1) / parts + kSpanTile - 1) / kSpanTile * kSpanTile;
+    const int chunk = ((longest + parts - 1) / parts + kSpanTile - 1) / kSpanTile * kSpanTile;  // of a wavefront
     const int64_t start = (int64_t)(split * W + wave) * chunk;
     const int j0 = __builtin_amdgcn_readfirstlane(start < nmax ? (int)start : nmax);
     const int j1 = __builtin_amdgcn_readfirstlane(nmax - j0 > chunk ? j0 + chunk : nmax);
     const int ntiles = (j1 - j0 + kSpanTile - 1) / kSpanTile;
 
-    // ---- Q^T operands: column c of tile nt = query row r0 + TR nt + c % TR; k-step s covers elements 32 s + 8 j + 0..7
-    f16x8_t qf[NT][KS], ql[RT ? NT : 1][RT ? KS : 1];
+    // ---- the query rows' loads are issued before the first tile's and converted behind them
+    f32x4_t qraw[NT][2 * KS];
     int lim[NT];
-    const float qscale = rsqrtf((float)HD) * 1.44269504f;
+    bool row_ok[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int rr = r0 + TR * nt + c % TR;
-        const bool ok = rr <= rlast;
-        const int rc = ok ? rr : rlast;
+        row_ok[nt] = rr <= rlast;
+        const int rc = row_ok[nt] ? rr : rlast;
         lim[nt] = limit(rc);
         const float *qp = a.q + (((size_t)b * a.T + rc / G) * a.Hq + kvh * G + rc % G) * HD + 8 * j;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            const f32x4_t x0 = *reinterpret_cast<const f32x4_t *>(qp + 32 * s), x1 = *reinterpret_cast<const f32x4_t *>(qp + 32 * s + 4);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = ok ? (e < 4 ? x0[e & 3] : x1[e & 3]) * qscale : 0.f;
-                const _Float16 hi = (_Float16)__builtin_amdgcn_fmed3f(v, -65504.f, 65504.f);  // saturating, like every half here
-                const _Float16 lo = (_Float16)__builtin_amdgcn_fmed3f(v - (float)hi, -65504.f, 65504.f);
-                qf[nt][s][e] = RT || c < 8 ? hi : lo;
-                if (RT) ql[RT ? nt : 0][RT ? s : 0][e] = lo;
-            }
+            qraw[nt][2 * s] = *reinterpret_cast<const f32x4_t *>(qp + 32 * s);
+            qraw[nt][2 * s + 1] = *reinterpret_cast<const f32x4_t *>(qp + 32 * s + 4);
         }
     }
 
     // ---- copies: instruction i of 16 rows moves rows (64 / LPR) i ..; this lane fills slot lane % LPR of row (64 / LPR) i + lane / LPR
     constexpr int CI = 16 * RB / 1024;
-    auto kperm = [](int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; };
     auto vperm = [](int r) { return HD == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); };
-    uint32_t ksrc[CI], vsrc[CI];
+    uint32_t vsrc[CI];
 #pragma unroll
     for (int i = 0; i < CI; ++i) {
         const int r = (64 / LPR) * i + lane / LPR, slot = lane % LPR;
-        ksrc[i] = (uint32_t)(r * RB + ((slot ^ kperm(r)) << 4));
         vsrc[i] = (uint32_t)(r * RB + ((slot ^ vperm(r)) << 4));
     }
     // Page numbers: 64 entries of the sequence's list in a register, one per lane (a load per tile would wait for the copies
@@ -168,9 +184,9 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
         const int page = __builtin_amdgcn_readlane(page_reg, at - page_base);
         return (((size_t)page * a.Hkv + kvh) << a.map.page_shift) + (row & ((1 << a.map.page_shift) - 1));
     };
-    auto issue_tile = [&](int tile, int stage) {
+    u32x4_t kreg[2][KS];                          // K operands of the next tile: row c of 16, elements 32 s + 8 j + 0..7
+    auto issue_tile = [&](int tile, unsigned char *st) {
         if (tile >= ntiles) return;
-        unsigned char *st = ring + stage * STAGE;
         size_t first[2];
         int rows[2];
 #pragma unroll
@@ -186,36 +202,52 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
             const size_t at = ((size_t)hi << 32 | lo) * HD;
             __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<f16_t *>(a.kc + at), 0, rows[h] * RB, 0x00020000);
             __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<f16_t *>(a.vc + at), 0, rows[h] * RB, 0x00020000);
+#if defined(__HIP_DEVICE_COMPILE__)  // the host pass does not know these builtins
 #pragma unroll
-            for (int i = 0; i < CI; ++i) {
-                unsigned char *kd = st + h * 16 * RB + i * 1024, *vd = kd + TILEB;
-#if defined(__HIP_DEVICE_COMPILE__)  // the host pass does not know this builtin
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, SPAN_LDS(kd), 16, (int)ksrc[i], 0, 0, ONCE ? 3 : 0);
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, SPAN_LDS(vd), 16, (int)vsrc[i], 0, 0, ONCE ? 3 : 0);
+            for (int s = 0; s < KS; ++s) kreg[h][s] = __builtin_amdgcn_raw_buffer_load_b128(kr, c * RB + (4 * s + j) * 16, 0, ONCE ? 3 : 0);
+#pragma unroll
+            for (int i = 0; i < CI; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, SPAN_LDS(st + h * 16 * RB + i * 1024), 16, (int)vsrc[i], 0, 0, ONCE ? 3 : 0);
 #else
-                (void)kd; (void)vd; (void)kr; (void)vr;
+            (void)kr; (void)vr;
 #endif
-            }
         }
         if (I16) {  // row scales: lane l takes row l % 32 (the tile's first row where there is none: its weight is 0)
             const int r = lane & 15, h = (lane >> 4) & 1;
             const size_t at = h ? (r < rows[1] ? first[1] + r : first[0]) : (r < rows[0] ? first[0] + r : first[0]);
 #if defined(__HIP_DEVICE_COMPILE__)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a.map.kscale + at), SPAN_LDS(st + 2 * TILEB), 4, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a.map.vscale + at), SPAN_LDS(st + 2 * TILEB + 256), 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a.map.kscale + at), SPAN_LDS(st + TILEB), 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a.map.vscale + at), SPAN_LDS(st + TILEB + 256), 4, 0, 0);
 #else
             (void)at;
 #endif
         }
     };
 
-    int kaddr[KS], vaddr[OT];
+    issue_tile(0, ring);
+    __builtin_amdgcn_sched_barrier(0);
+
+    // ---- Q^T operands: column c of tile nt = query row r0 + TR nt + c % TR; k-step s covers elements 32 s + 8 j + 0..7
+    f16x8_t qf[NT][KS], ql[RT ? NT : 1][RT ? KS : 1];
+    const float qscale = rsqrtf((float)HD) * 1.44269504f;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) kaddr[s] = c * RB + (((4 * s + j) ^ kperm(c)) << 4);
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = row_ok[nt] ? qraw[nt][2 * s + (e >> 2)][e & 3] * qscale : 0.f;
+                const _Float16 hi = (_Float16)__builtin_amdgcn_fmed3f(v, -65504.f, 65504.f);  // saturating, like every half here
+                const _Float16 lo = (_Float16)__builtin_amdgcn_fmed3f(v - (float)hi, -65504.f, 65504.f);
+                qf[nt][s][e] = RT || c < 8 ? hi : lo;
+                if (RT) ql[RT ? nt : 0][RT ? s : 0][e] = lo;
+            }
+
+    int vaddr[OT];
     {
         const int r = 4 * j + (c >> 2);  // the row whose 4 elements this lane hands to the transposing read
 #pragma unroll
-        for (int t = 0; t < OT; ++t) vaddr[t] = TILEB + r * RB + (((2 * t + ((c >> 1) & 1)) ^ vperm(r)) << 4) + 8 * (c & 1);
+        for (int t = 0; t < OT; ++t) vaddr[t] = r * RB + (((2 * t + ((c >> 1) & 1)) ^ vperm(r)) << 4) + 8 * (c & 1);
     }
 
     f32x4_t acc[NT][OT];
@@ -226,11 +258,11 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
 #pragma unroll
         for (int t = 0; t < OT; ++t) acc[nt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    const SpanWs w = span_ws(a.B, a.T, a.Hq, HD, a.S, a.nsplit, a.weight != nullptr);
+    const SpanWs w = span_ws(a.B, a.T, a.Hq, a.Hkv, HD, a.S, a.nsplit, WT);
     const size_t row_base = ((size_t)b * a.Hkv + kvh) * a.T * G;  // query rows in the workspace: [b][kv head][t * G + g]
-    float *scores = a.ws + w.scores + row_base * w.ld;
+    float *scores = a.ws + w.scores + ((size_t)b * a.Hkv + kvh) * w.slab + (size_t)rt * w.tiles * (ROWS * kSpanTile);
 
-    auto consume = [&](int tile, unsigned char *st) {
+    auto consume = [&](int tile, unsigned char *st, unsigned char *other) {
         const int key0 = j0 + tile * kSpanTile;
         f32x4_t sacc[NT][2];
 #pragma unroll
@@ -239,7 +271,7 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                const u32x4_t kw = *reinterpret_cast<const u32x4_t *>(st + h * 16 * RB + kaddr[s]);
+                const u32x4_t kw = kreg[h][s];
                 f16x8_t kh, kl;
                 if (I16) span_split(kw, &kh, &kl);
                 else kh = __builtin_bit_cast(f16x8_t, kw);
@@ -255,10 +287,13 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
         if (I16) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                ksc[h] = *reinterpret_cast<const f32x4_t *>(st + 2 * TILEB + 64 * h + 16 * j);
-                vsc[h] = *reinterpret_cast<const f32x4_t *>(st + 2 * TILEB + 256 + 64 * h + 16 * j);
+                ksc[h] = *reinterpret_cast<const f32x4_t *>(st + TILEB + 64 * h + 16 * j);
+                vsc[h] = *reinterpret_cast<const f32x4_t *>(st + TILEB + 256 + 64 * h + 16 * j);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        issue_tile(tile + 1, other);              // K into the registers just used, V into the stage consumed one step ago
+        __builtin_amdgcn_sched_barrier(0);
         const bool tail = key0 + kSpanTile > nmin || key0 + kSpanTile > j1;  // some query row does not see all of these keys
         if (!I16 && tail) {
             // A value that is not finite must not reach the query rows that do not see its row (0 * inf is NaN): such elements are
@@ -266,7 +301,7 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
             bool bad = false;
 #pragma unroll
             for (int i = 0; i < TILEB / 1024; ++i) {
-                const u32x4_t x = *reinterpret_cast<const u32x4_t *>(st + TILEB + i * 1024 + lane * 16);
+                const u32x4_t x = *reinterpret_cast<const u32x4_t *>(st + i * 1024 + lane * 16);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7c00u) == 0x7c00u || (x[e] & 0x7c000000u) == 0x7c000000u;
             }
@@ -277,7 +312,7 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const int e = 16 * t + 4 * j + i, kr = k & 15;
-                            f16_t *p = reinterpret_cast<f16_t *>(st + TILEB + k * RB + (((e >> 3) ^ vperm(kr)) << 4) + (e & 7) * 2);
+                            f16_t *p = reinterpret_cast<f16_t *>(st + k * RB + (((e >> 3) ^ vperm(kr)) << 4) + (e & 7) * 2);
                             const f16_t v = *p;
                             if ((v & 0x7c00u) == 0x7c00u) {
 #pragma unroll
@@ -288,7 +323,7 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
                 for (int i = 0; i < TILEB / 1024; ++i) {
-                    u32x4_t *p = reinterpret_cast<u32x4_t *>(st + TILEB + i * 1024 + lane * 16);
+                    u32x4_t *p = reinterpret_cast<u32x4_t *>(st + i * 1024 + lane * 16);
                     u32x4_t x = *p;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -316,10 +351,14 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
                 for (int e = 0; e < 8; ++e)
                     if (key0 + 16 * (e >> 2) + 4 * j + (e & 3) >= (lim[nt] < j1 ? lim[nt] : j1)) v[e] = -INFINITY;
             }
-            if (a.weight && (RT || c < 8) && r0 + TR * nt + c <= rlast) {
-                float *sp = scores + (size_t)(r0 + TR * nt + c) * w.ld + key0 + 4 * j;
-                *reinterpret_cast<f32x4_t *>(sp) = f32x4_t{v[0], v[1], v[2], v[3]};
-                *reinterpret_cast<f32x4_t *>(sp + 16) = f32x4_t{v[4], v[5], v[6], v[7]};
+            if (WT) {                             // lanes of the low term store the second 16 keys
+                float *sp = scores + (size_t)(key0 / kSpanTile) * (ROWS * kSpanTile) + (TR * nt + c % TR) * kSpanTile + 4 * j;
+                if (RT) {
+                    *reinterpret_cast<f32x4_t *>(sp) = f32x4_t{v[0], v[1], v[2], v[3]};
+                    *reinterpret_cast<f32x4_t *>(sp + 16) = f32x4_t{v[4], v[5], v[6], v[7]};
+                } else {
+                    *reinterpret_cast<f32x4_t *>(sp + (c < 8 ? 0 : 16)) = c < 8 ? f32x4_t{v[0], v[1], v[2], v[3]} : f32x4_t{v[4], v[5], v[6], v[7]};
+                }
             }
             float tmax = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
             if (__any(tmax > mrun[nt] + kSpanSlack)) {
@@ -404,32 +443,23 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
         }
     };
 
-#pragma unroll
-    for (int k = 0; k < NST - 1; ++k) issue_tile(k, k);
-    __builtin_amdgcn_sched_barrier(0);
-    // A tile has landed once at most the copies of NST - 2 younger tiles are pending; the score stores between them count too, so
-    // with weights everything is waited for (as at the end, where fewer tiles are in flight).
-    constexpr int YOUNGER = (4 * CI + (I16 ? 2 : 0)) * (NST - 2);
-    static_assert(YOUNGER < 64, "vmcnt is a 6-bit counter");
-    for (int tile = 0, stage = 0; tile < ntiles; ++tile) {
-        if (YOUNGER > 0 && !a.weight && tile + NST - 2 < ntiles)
-            __builtin_amdgcn_s_waitcnt((YOUNGER & 15) | (7 << 4) | (15 << 8) | ((YOUNGER >> 4) << 14));  // vmcnt(YOUNGER) only
-        else
-            __builtin_amdgcn_s_waitcnt((0 & 15) | (7 << 4) | (15 << 8) | (0 << 14));                     // vmcnt(0)
+    constexpr int STORES = RT ? 2 * NT : 1;       // of scores, issued behind the next tile's copies: they need not have arrived
+    for (int tile = 0; tile < ntiles; ++tile) {
+        unsigned char *st = ring + (tile & 1) * STAGE;
         __builtin_amdgcn_sched_barrier(0);
-        const int free_stage = stage == 0 ? NST - 1 : stage - 1;  // the stage consumed one step ago
-        issue_tile(tile + NST - 1, free_stage);
+        // the tile has landed once nothing older than those stores is pending: vmcnt(0) or (STORES) only
+        if (tile == 0 || !WT) __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));
+        else __builtin_amdgcn_s_waitcnt(STORES | (7 << 4) | (15 << 8));
         __builtin_amdgcn_sched_barrier(0);
-        consume(tile, ring + stage * STAGE);
-        __builtin_amdgcn_sched_barrier(0);
-        stage = stage == NST - 1 ? 0 : stage + 1;
+        consume(tile, st, ring + (~tile & 1) * STAGE);
     }
+    __builtin_amdgcn_sched_barrier(0);
 
     // ---- join the wavefronts: the lane groups j hold disjoint keys (den), columns c and c + 8 the two terms of a query row (acc)
     // over the wavefront's ring (all copies have landed): [ROWS][HD] sums, [ROWS] maxima, [ROWS] denominators
     float *part = reinterpret_cast<float *>(ring);
-    auto s_max = [&](int i, int r) -> float & { return reinterpret_cast<float *>(ring_all + i * (NST * STAGE))[ROWS * HD + r]; };
-    auto s_den = [&](int i, int r) -> float & { return reinterpret_cast<float *>(ring_all + i * (NST * STAGE))[ROWS * (HD + 1) + r]; };
+    auto s_max = [&](int i, int r) -> float & { return reinterpret_cast<float *>(ring_all + i * (OWN))[ROWS * HD + r]; };
+    auto s_den = [&](int i, int r) -> float & { return reinterpret_cast<float *>(ring_all + i * (OWN))[ROWS * (HD + 1) + r]; };
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         float d = den[nt];
@@ -445,7 +475,9 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
             if (c < TR) *reinterpret_cast<f32x4_t *>(part + (TR * nt + c) * HD + 16 * t + 4 * j) = o;
         }
     }
+    __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));  // the score stores have arrived
     __syncthreads();
+    const bool weigh = ONCE && WT && a.nsplit == 1;  // this workgroup has seen all queries and rows of its kv head
     constexpr int TPR = HD / 8;                     // threads per query row, 8 elements each
     for (int r = threadIdx.x / TPR; r < ROWS && r0 + r <= rlast; r += 64 * W / TPR) {
         const int e0 = (threadIdx.x % TPR) * 8;
@@ -458,13 +490,15 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
             const float f = s_max(i, r) == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_max(i, r) - m);
             if (s_max(i, r) == -INFINITY && !(s_den(i, r) != s_den(i, r))) continue;  // a part without visible keys
             d += s_den(i, r) * f;
-            const float *p = reinterpret_cast<const float *>(ring_all + i * (NST * STAGE)) + r * HD + e0;
+            const float *p = reinterpret_cast<const float *>(ring_all + i * (OWN)) + r * HD + e0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] += p[e] * f;
         }
         const int rr = r0 + r;
         const size_t row = row_base + rr;
-        if (a.nsplit > 1 || a.weight) {
+        if (weigh) {
+            if (e0 == 0) { s_rows[0][r] = m; s_rows[1][r] = 1.0f / d; }
+        } else if (a.nsplit > 1 || WT) {
             if (e0 == 0) {
                 a.ws[w.stats + (row * a.nsplit + split) * 2] = m;
                 a.ws[w.stats + (row * a.nsplit + split) * 2 + 1] = d;
@@ -487,14 +521,55 @@ __global__ __launch_bounds__(64 * W) void span_attention_kernel(SpanArgs a, int 
             if (a.out_lo) *reinterpret_cast<u32x4_t *>(a.out_lo + at) = l;
         }
     }
+    if (weigh) {
+        __syncthreads();
+        float *wt = a.weight + ((size_t)b * a.Hkv + kvh) * a.S;
+        constexpr int STEP = 256 * W;
+        auto pass = [&](auto two, int key) {      // 4 keys of a thread, or 4 and 4 a step apart: all loads of 8 query rows in flight
+            constexpr int P = decltype(two)::value ? 2 : 1;
+            float sum[P][4], old[P][4];
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { sum[p][i] = 0.f; old[p][i] = key + p * STEP + i < nmax ? wt[key + p * STEP + i] : 0.f; }
+            for (int rb = 0; rb <= rlast; rb += 8) {
+                f32x4_t x[P][8];
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {  // rows behind the last one are part of the block
+                        const int k = key + p * STEP;
+                        x[p][r] = k < nmax ? *reinterpret_cast<const f32x4_t *>(scores + (size_t)(k / kSpanTile) * (ROWS * kSpanTile) + (rb + r) * kSpanTile + k % kSpanTile) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+                    }
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    if (rb + r > rlast) break;
+                    const int last = limit(rb + r);
+                    const float m = s_rows[0][rb + r], inv = s_rows[1][rb + r];
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sum[p][i] += key + p * STEP + i < last ? __builtin_amdgcn_exp2f(x[p][r][i] - m) * inv : 0.f;
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (key + p * STEP + i < nmax) wt[key + p * STEP + i] = old[p][i] + sum[p][i];
+        };
+        int key = threadIdx.x * 4, left = nmax;   // the last threads' keys of a pass decide how many steps it takes
+        for (; left > STEP; left -= 2 * STEP, key += 2 * STEP) pass(std::true_type(), key);
+        if (left > 0) pass(std::false_type(), key);
+    }
 }
 
-// Second launch: the first `merge_blocks` workgroups join the splits of 4 query rows each (a wavefront per row), the others add up
+// Second launch, where the rows of a sequence or its queries are on several workgroups: the first `merge_blocks` workgroups join the splits of 4 query rows each (a wavefront per row), the others add up
 // the weights of 1024 cache rows of a (sequence, kv head) each: exp2(score - max) / sum over the query rows, in their order.
 __global__ __launch_bounds__(256) void span_join_kernel(SpanArgs a, int merge_blocks, int key_blocks) {
     __shared__ float s_m[256], s_inv[256];
-    const SpanWs w = span_ws(a.B, a.T, a.Hq, a.hd, a.S, a.nsplit, a.weight != nullptr);
-    const int G = a.Hq / a.Hkv;
+    const SpanWs w = span_ws(a.B, a.T, a.Hq, a.Hkv, a.hd, a.S, a.nsplit, a.weight != nullptr);
+    const int G = a.Hq / a.Hkv, per_wg = span_rows(a.T, G);
     if ((int)blockIdx.x < merge_blocks) {
         const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
         const int lane = threadIdx.x & 63;
@@ -538,7 +613,7 @@ __global__ __launch_bounds__(256) void span_join_kernel(SpanArgs a, int merge_bl
     const int n = n0 + tn < a.S ? n0 + tn : a.S;  // rows that the last token sees
     if (tn == 0 || (blk % key_blocks) * 1024 >= n) return;
     const size_t row0 = (size_t)slab * a.T * G;
-    const float *sc = a.ws + w.scores + row0 * w.ld + key;
+    const float *sc = a.ws + w.scores + (size_t)slab * w.slab + (size_t)(key / kSpanTile) * (per_wg * kSpanTile) + key % kSpanTile;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     for (int rr0 = 0; rr0 < tn * G; rr0 += 256) {
         __syncthreads();
@@ -559,7 +634,8 @@ __global__ __launch_bounds__(256) void span_join_kernel(SpanArgs a, int merge_bl
             for (int r = 0; r < count; ++r) {
                 int lim = n0 + (rr0 + r) / G + 1;
                 lim = lim < a.S ? lim : a.S;
-                const f32x4_t s = *reinterpret_cast<const f32x4_t *>(sc + (size_t)(rr0 + r) * w.ld);
+                const int rr = rr0 + r;
+                const f32x4_t s = *reinterpret_cast<const f32x4_t *>(sc + (size_t)(rr / per_wg) * w.tiles * (per_wg * kSpanTile) + rr % per_wg * kSpanTile);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (key + i < lim) sum[i] += __builtin_amdgcn_exp2f(s[i] - s_m[r]) * s_inv[r];
@@ -571,11 +647,6 @@ __global__ __launch_bounds__(256) void span_join_kernel(SpanArgs a, int merge_bl
         if (key + i < n) wt[i] += sum[i];
 }
 
-// Query rows of a workgroup.
-static int span_rows(int T, int G) {
-    const int64_t R = (int64_t)T * G;
-    return R <= 8 ? 8 : R <= 16 ? 16 : 32;
-}
 static int64_t span_items(int B, int T, int Hq, int Hkv) {
     const int G = Hq / Hkv, rows = span_rows(T, G);
     return (int64_t)B * Hkv * ((T * (int64_t)G + rows - 1) / rows);
@@ -583,7 +654,7 @@ static int64_t span_items(int B, int T, int Hq, int Hkv) {
 
 int span_attention_splits(int B, int T, int Hq, int Hkv, int hd, int S) {
     const int64_t items = span_items(B, T, Hq, Hkv);
-    int64_t s = items > 0 ? 256 / items : 1;         // one workgroup per compute unit
+    int64_t s = items > 0 ? 512 / items : 1;         // two workgroups of four wavefronts per compute unit
     const int cap = S / 512;                          // each with 512 rows at least at full length
     if (s > cap) s = cap;
     if (s > 64) s = 64;
@@ -591,18 +662,19 @@ int span_attention_splits(int B, int T, int Hq, int Hkv, int hd, int S) {
 }
 
 size_t span_attention_ws_floats(int B, int T, int Hq, int Hkv, int hd, int S, int nsplit, bool weights) {
-    return span_ws(B, T, Hq, hd, S, nsplit, weights).total;
+    return span_ws(B, T, Hq, Hkv, hd, S, nsplit, weights).total;
 }
 
 template <int HD, int RT, bool I16, bool ONCE>
 static void span_launch(const SpanArgs &a, int row_tiles, hipStream_t st) {
     const int items = a.B * a.Hkv * a.nsplit;
     const unsigned blocks = (unsigned)((int64_t)ceil_div(items, 8) * 8 * row_tiles);
-    // wavefronts that share a sequence's rows: enough of them for the compute units when there are few items
-    const int64_t work = (int64_t)items * row_tiles;
-    if (work <= 256) span_attention_kernel<HD, RT, 4, I16, ONCE><<<blocks, 256, 0, st>>>(a, row_tiles, items);
-    else if (work <= 512) span_attention_kernel<HD, RT, 2, I16, ONCE><<<blocks, 128, 0, st>>>(a, row_tiles, items);
-    else span_attention_kernel<HD, RT, 1, I16, ONCE><<<blocks, 64, 0, st>>>(a, row_tiles, items);
+    // wavefronts that share a sequence's rows: four where that does not make more workgroups than run at once (two per compute unit)
+    const bool four = (int64_t)items * row_tiles <= 512;
+    if (four && a.weight) span_attention_kernel<HD, RT, 4, I16, ONCE, true><<<blocks, 256, 0, st>>>(a, row_tiles, items);
+    else if (four) span_attention_kernel<HD, RT, 4, I16, ONCE, false><<<blocks, 256, 0, st>>>(a, row_tiles, items);
+    else if (a.weight) span_attention_kernel<HD, RT, 2, I16, ONCE, true><<<blocks, 128, 0, st>>>(a, row_tiles, items);
+    else span_attention_kernel<HD, RT, 2, I16, ONCE, false><<<blocks, 128, 0, st>>>(a, row_tiles, items);
 }
 template <int HD, bool I16>
 static void span_launch_tiles(const SpanArgs &a, hipStream_t st) {
@@ -618,7 +690,8 @@ void launch_span_attention(const SpanArgs &a, hipStream_t st) {
     if (a.hd == 128) a.map.kscale ? span_launch_tiles<128, true>(a, st) : span_launch_tiles<128, false>(a, st);
     else a.map.kscale ? span_launch_tiles<64, true>(a, st) : span_launch_tiles<64, false>(a, st);
     const int merge_blocks = a.nsplit > 1 ? (int)(((int64_t)a.B * a.T * a.Hq + 3) / 4) : 0;
-    const int key_blocks = a.weight ? ceil_div(a.S, 1024) : 0;
+    const bool several = a.nsplit > 1 || (int64_t)a.T * (a.Hq / a.Hkv) > 32;
+    const int key_blocks = a.weight && several ? ceil_div(a.S, 1024) : 0;
     const int64_t blocks = merge_blocks + (int64_t)a.B * a.Hkv * key_blocks;
     if (blocks > 0) span_join_kernel<<<(unsigned)blocks, 256, 0, st>>>(a, merge_blocks, key_blocks ? key_blocks : 1);
 }
