@@ -86,11 +86,12 @@ __device__ __forceinline__ void span_extent(const SpanArgs &a, int b, int *n0, i
 // RT: 0: 8 query rows with both terms in one tile; 1, 2: so many tiles of 16 rows.
 // WT: the scores are kept and the weights added up.
 template <int HD, int RT, int W, bool I16, bool ONCE, bool WT>
-__global__ __launch_bounds__(64 * W, 2) void span_attention_kernel(SpanArgs a, int row_tiles, int items) {
+__global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel(SpanArgs a, int row_tiles, int items) {
     constexpr int RB = HD * 2;                    // bytes of a cache row
     constexpr int KS = HD / 32, OT = HD / 16;     // k-steps of a score, tiles of the output
     constexpr int TILEB = kSpanTile * RB;
-    constexpr int STAGE = TILEB + (I16 ? 512 : 0);  // a V tile and the row scales of K and V
+    constexpr bool KL = RT == 2;                  // K through LDS as well
+    constexpr int SCALES = KL ? 2 * TILEB : TILEB, STAGE = SCALES + (I16 ? 512 : 0);  // a V tile, with KL a K tile, the row scales of K and V
     constexpr int LPR = RB / 16;                  // lanes per row of a copy instruction
     constexpr int NT = RT ? RT : 1, TR = RT ? 16 : 8, ROWS = TR * NT;  // column tiles, query rows of a tile and of this workgroup
     constexpr int OWN = 2 * STAGE > ROWS * (HD + 2) * 4 ? 2 * STAGE : (ROWS * (HD + 2) * 4 + 1023) / 1024 * 1024;  // LDS of a wavefront
@@ -158,11 +159,13 @@ __global__ __launch_bounds__(64 * W, 2) void span_attention_kernel(SpanArgs a, i
     // ---- copies: instruction i of 16 rows moves rows (64 / LPR) i ..; this lane fills slot lane % LPR of row (64 / LPR) i + lane / LPR
     constexpr int CI = 16 * RB / 1024;
     auto vperm = [](int r) { return HD == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); };
-    uint32_t vsrc[CI];
+    auto kperm = [](int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; };
+    uint32_t vsrc[CI], ksrc[KL ? CI : 1];
 #pragma unroll
     for (int i = 0; i < CI; ++i) {
         const int r = (64 / LPR) * i + lane / LPR, slot = lane % LPR;
         vsrc[i] = (uint32_t)(r * RB + ((slot ^ vperm(r)) << 4));
+        if (KL) ksrc[KL ? i : 0] = (uint32_t)(r * RB + ((slot ^ kperm(r)) << 4));
     }
     // Page numbers: 64 entries of the sequence's list in a register, one per lane (a load per tile would wait for the copies
     // in flight, which return in order).
@@ -184,7 +187,7 @@ __global__ __launch_bounds__(64 * W, 2) void span_attention_kernel(SpanArgs a, i
         const int page = __builtin_amdgcn_readlane(page_reg, at - page_base);
         return (((size_t)page * a.Hkv + kvh) << a.map.page_shift) + (row & ((1 << a.map.page_shift) - 1));
     };
-    u32x4_t kreg[2][KS];                          // K operands of the next tile: row c of 16, elements 32 s + 8 j + 0..7
+    u32x4_t kreg[KL ? 1 : 2][KL ? 1 : KS];                          // K operands of the next tile: row c of 16, elements 32 s + 8 j + 0..7
     auto issue_tile = [&](int tile, unsigned char *st) {
         if (tile >= ntiles) return;
         size_t first[2];
@@ -204,7 +207,11 @@ __global__ __launch_bounds__(64 * W, 2) void span_attention_kernel(SpanArgs a, i
             __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<f16_t *>(a.vc + at), 0, rows[h] * RB, 0x00020000);
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass does not know these builtins
 #pragma unroll
-            for (int s = 0; s < KS; ++s) kreg[h][s] = __builtin_amdgcn_raw_buffer_load_b128(kr, c * RB + (4 * s + j) * 16, 0, ONCE ? 3 : 0);
+            for (int s = 0; s < KS; ++s)
+                if (!KL) kreg[KL ? 0 : h][KL ? 0 : s] = __builtin_amdgcn_raw_buffer_load_b128(kr, c * RB + (4 * s + j) * 16, 0, ONCE ? 3 : 0);
+#pragma unroll
+            for (int i = 0; i < CI; ++i)
+                if (KL) __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, SPAN_LDS(st + TILEB + h * 16 * RB + i * 1024), 16, (int)ksrc[KL ? i : 0], 0, 0, ONCE ? 3 : 0);
 #pragma unroll
             for (int i = 0; i < CI; ++i)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, SPAN_LDS(st + h * 16 * RB + i * 1024), 16, (int)vsrc[i], 0, 0, ONCE ? 3 : 0);
@@ -216,8 +223,8 @@ __global__ __launch_bounds__(64 * W, 2) void span_attention_kernel(SpanArgs a, i
             const int r = lane & 15, h = (lane >> 4) & 1;
             const size_t at = h ? (r < rows[1] ? first[1] + r : first[0]) : (r < rows[0] ? first[0] + r : first[0]);
 #if defined(__HIP_DEVICE_COMPILE__)
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a.map.kscale + at), SPAN_LDS(st + TILEB), 4, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a.map.vscale + at), SPAN_LDS(st + TILEB + 256), 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a.map.kscale + at), SPAN_LDS(st + SCALES), 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a.map.vscale + at), SPAN_LDS(st + SCALES + 256), 4, 0, 0);
 #else
             (void)at;
 #endif
@@ -243,7 +250,10 @@ __global__ __launch_bounds__(64 * W, 2) void span_attention_kernel(SpanArgs a, i
                 if (RT) ql[RT ? nt : 0][RT ? s : 0][e] = lo;
             }
 
-    int vaddr[OT];
+    int vaddr[OT], kaddr[KL ? KS : 1];
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+        if (KL) kaddr[KL ? s : 0] = c * RB + (((4 * s + j) ^ kperm(c)) << 4);
     {
         const int r = 4 * j + (c >> 2);  // the row whose 4 elements this lane hands to the transposing read
 #pragma unroll
@@ -264,6 +274,8 @@ __global__ __launch_bounds__(64 * W, 2) void span_attention_kernel(SpanArgs a, i
 
     auto consume = [&](int tile, unsigned char *st, unsigned char *other) {
         const int key0 = j0 + tile * kSpanTile;
+        if (KL) issue_tile(tile + 1, other);      // into the stage consumed one step ago
+        __builtin_amdgcn_sched_barrier(0);
         f32x4_t sacc[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) sacc[nt][0] = sacc[nt][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -271,7 +283,7 @@ __global__ __launch_bounds__(64 * W, 2) void span_attention_kernel(SpanArgs a, i
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                const u32x4_t kw = kreg[h][s];
+                const u32x4_t kw = KL ? *reinterpret_cast<const u32x4_t *>(st + TILEB + h * 16 * RB + kaddr[KL ? s : 0]) : kreg[KL ? 0 : h][KL ? 0 : s];
                 f16x8_t kh, kl;
                 if (I16) span_split(kw, &kh, &kl);
                 else kh = __builtin_bit_cast(f16x8_t, kw);
@@ -287,12 +299,12 @@ __global__ __launch_bounds__(64 * W, 2) void span_attention_kernel(SpanArgs a, i
         if (I16) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                ksc[h] = *reinterpret_cast<const f32x4_t *>(st + TILEB + 64 * h + 16 * j);
-                vsc[h] = *reinterpret_cast<const f32x4_t *>(st + TILEB + 256 + 64 * h + 16 * j);
+                ksc[h] = *reinterpret_cast<const f32x4_t *>(st + SCALES + 64 * h + 16 * j);
+                vsc[h] = *reinterpret_cast<const f32x4_t *>(st + SCALES + 256 + 64 * h + 16 * j);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        issue_tile(tile + 1, other);              // K into the registers just used, V into the stage consumed one step ago
+        if (!KL) issue_tile(tile + 1, other);              // K into the registers just used, V into the stage consumed one step ago
         __builtin_amdgcn_sched_barrier(0);
         const bool tail = key0 + kSpanTile > nmin || key0 + kSpanTile > j1;  // some query row does not see all of these keys
         if (!I16 && tail) {
@@ -564,11 +576,13 @@ __global__ __launch_bounds__(64 * W, 2) void span_attention_kernel(SpanArgs a, i
     }
 }
 
-// Second launch, where the rows of a sequence or its queries are on several workgroups: the first `merge_blocks` workgroups join the splits of 4 query rows each (a wavefront per row), the others add up
-// the weights of 1024 cache rows of a (sequence, kv head) each: exp2(score - max) / sum over the query rows, in their order.
+// Second launch, where the rows of a sequence or its queries are on several workgroups: the first `merge_blocks` workgroups join the
+// splits of 4 query rows each (a wavefront per row, a lane per split's statistics), the others add up the weights of 1024 cache rows of
+// a (sequence, kv head) each: exp2(score - max) / sum over the query rows, in their order.
+template <int HD>
 __global__ __launch_bounds__(256) void span_join_kernel(SpanArgs a, int merge_blocks, int key_blocks) {
     __shared__ float s_m[256], s_inv[256];
-    const SpanWs w = span_ws(a.B, a.T, a.Hq, a.Hkv, a.hd, a.S, a.nsplit, a.weight != nullptr);
+    const SpanWs w = span_ws(a.B, a.T, a.Hq, a.Hkv, HD, a.S, a.nsplit, a.weight != nullptr);
     const int G = a.Hq / a.Hkv, per_wg = span_rows(a.T, G);
     if ((int)blockIdx.x < merge_blocks) {
         const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -580,21 +594,36 @@ __global__ __launch_bounds__(256) void span_join_kernel(SpanArgs a, int merge_bl
         span_extent(a, b, &n0, &tn);
         if (rr >= tn * G) return;
         const float *st = a.ws + w.stats + row * a.nsplit * 2;
-        float m = -INFINITY;
-        for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, st[2 * s]);
-        float d = 0.f, o0 = 0.f, o1 = 0.f;
-        const int per = a.hd / 64;
-        for (int s = 0; s < a.nsplit; ++s) {
-            if (st[2 * s] == -INFINITY && !(st[2 * s + 1] != st[2 * s + 1])) continue;
-            const float f = st[2 * s] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[2 * s] - m);
-            d += st[2 * s + 1] * f;
-            const float *p = a.ws + w.part + (row * a.nsplit + s) * a.hd + lane * per;
-            o0 += p[0] * f;
-            if (per == 2) o1 += p[1] * f;
+        constexpr int PER = HD / 64;
+        const float *p = a.ws + w.part + row * a.nsplit * HD + lane * PER;
+        const float pm = lane < a.nsplit ? st[2 * lane] : -INFINITY, pd = lane < a.nsplit ? st[2 * lane + 1] : 0.f;
+        float x[8][PER];                          // parts of 8 splits in flight
+        auto fetch = [&](int s0) {
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+#pragma unroll
+                for (int e = 0; e < PER; ++e) x[s][e] = s0 + s < a.nsplit ? p[(s0 + s) * HD + e] : 0.f;
+        };
+        fetch(0);
+        float m = pm;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+        const float f = pm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(pm - m);
+        float d = pd * f, o0 = 0.f, o1 = 0.f;     // (a split without visible rows has zeros throughout)
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) d += __shfl_xor(d, o, 64);
+        for (int s0 = 0; s0 < a.nsplit; s0 += 8) {
+            if (s0) fetch(s0);
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                const float fs = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), (s0 + s) & 63));
+                o0 += x[s][0] * fs;
+                if (PER == 2) o1 += x[s][PER - 1] * fs;
+            }
         }
         const float inv = 1.0f / d;
-        const size_t at = (((size_t)b * a.T + rr / G) * a.Hq + kvh * G + rr % G) * a.hd + lane * per;
-        if (per == 2) {
+        const size_t at = (((size_t)b * a.T + rr / G) * a.Hq + kvh * G + rr % G) * HD + lane * PER;
+        if (PER == 2) {
             const uint32_t h = pack_f16x2(o0 * inv, o1 * inv);
             *reinterpret_cast<uint32_t *>(a.out + at) = h;
             if (a.out_lo) *reinterpret_cast<uint32_t *>(a.out_lo + at) = pack_f16x2_lo(o0 * inv, o1 * inv, h);
@@ -621,7 +650,9 @@ __global__ __launch_bounds__(256) void span_join_kernel(SpanArgs a, int merge_bl
         if (mine < tn * G) {
             const float *st = a.ws + w.stats + (row0 + mine) * a.nsplit * 2;
             float m = -INFINITY, d = 0.f;
+#pragma unroll 8
             for (int s = 0; s < a.nsplit; ++s) m = fmaxf(m, st[2 * s]);
+#pragma unroll 8
             for (int s = 0; s < a.nsplit; ++s)
                 if (st[2 * s] != -INFINITY || st[2 * s + 1] != st[2 * s + 1]) d += st[2 * s + 1] * __builtin_amdgcn_exp2f(st[2 * s] - m);
             s_m[threadIdx.x] = m;
@@ -654,7 +685,7 @@ static int64_t span_items(int B, int T, int Hq, int Hkv) {
 
 int span_attention_splits(int B, int T, int Hq, int Hkv, int hd, int S) {
     const int64_t items = span_items(B, T, Hq, Hkv);
-    int64_t s = items > 0 ? 512 / items : 1;         // two workgroups of four wavefronts per compute unit
+    int64_t s = items > 0 ? (span_rows(T, Hq / Hkv) == 32 ? 256 : 512) / items : 1;         // two workgroups of four wavefronts per compute unit
     const int cap = S / 512;                          // each with 512 rows at least at full length
     if (s > cap) s = cap;
     if (s > 64) s = 64;
@@ -693,5 +724,5 @@ void launch_span_attention(const SpanArgs &a, hipStream_t st) {
     const bool several = a.nsplit > 1 || (int64_t)a.T * (a.Hq / a.Hkv) > 32;
     const int key_blocks = a.weight && several ? ceil_div(a.S, 1024) : 0;
     const int64_t blocks = merge_blocks + (int64_t)a.B * a.Hkv * key_blocks;
-    if (blocks > 0) span_join_kernel<<<(unsigned)blocks, 256, 0, st>>>(a, merge_blocks, key_blocks ? key_blocks : 1);
+    if (blocks > 0) (a.hd == 128 ? span_join_kernel<128> : span_join_kernel<64>)<<<(unsigned)blocks, 256, 0, st>>>(a, merge_blocks, key_blocks ? key_blocks : 1);
 }
