@@ -91,6 +91,7 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
     constexpr int KS = HD / 32, OT = HD / 16;     // k-steps of a score, tiles of the output
     constexpr int TILEB = kSpanTile * RB;
     constexpr bool KL = RT == 2;                  // K through LDS as well
+    constexpr bool EARLY = KL || !WT;
     constexpr int SCALES = KL ? 2 * TILEB : TILEB, STAGE = SCALES + (I16 ? 512 : 0);  // a V tile, with KL a K tile, the row scales of K and V
     constexpr int LPR = RB / 16;                  // lanes per row of a copy instruction
     constexpr int NT = RT ? RT : 1, TR = RT ? 16 : 8, ROWS = TR * NT;  // column tiles, query rows of a tile and of this workgroup
@@ -188,10 +189,15 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
         return (((size_t)page * a.Hkv + kvh) << a.map.page_shift) + (row & ((1 << a.map.page_shift) - 1));
     };
     u32x4_t kreg[KL ? 1 : 2][KL ? 1 : KS];                          // K operands of the next tile: row c of 16, elements 32 s + 8 j + 0..7
-    auto issue_tile = [&](int tile, unsigned char *st) {
+    size_t first[2];                              // of the tile that is being copied: where its two blocks of 16 rows are, how many exist
+    int rows[2];
+    auto piece = [&](const f16_t *base, int h) {
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)first[h]), hi = __builtin_amdgcn_readfirstlane((uint32_t)(first[h] >> 32));
+        const size_t at = ((size_t)hi << 32 | lo) * HD;
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<f16_t *>(base + at), 0, rows[h] * RB, 0x00020000);
+    };
+    auto issue_v = [&](int tile, unsigned char *st) {  // V, row scales, and K where it goes through LDS
         if (tile >= ntiles) return;
-        size_t first[2];
-        int rows[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int row0 = j0 + tile * kSpanTile + 16 * h;
@@ -199,39 +205,44 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
             rows[h] = __builtin_amdgcn_readfirstlane(rows[h] < 0 ? 0 : (rows[h] > 16 ? 16 : rows[h]));
             first[h] = rows[h] ? row_of(row0) : first[0];
         }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)first[h]), hi = __builtin_amdgcn_readfirstlane((uint32_t)(first[h] >> 32));
-            const size_t at = ((size_t)hi << 32 | lo) * HD;
-            __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<f16_t *>(a.kc + at), 0, rows[h] * RB, 0x00020000);
-            __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<f16_t *>(a.vc + at), 0, rows[h] * RB, 0x00020000);
 #if defined(__HIP_DEVICE_COMPILE__)  // the host pass does not know these builtins
 #pragma unroll
-            for (int s = 0; s < KS; ++s)
-                if (!KL) kreg[KL ? 0 : h][KL ? 0 : s] = __builtin_amdgcn_raw_buffer_load_b128(kr, c * RB + (4 * s + j) * 16, 0, ONCE ? 3 : 0);
+        for (int h = 0; h < 2; ++h) {
+            __amdgpu_buffer_rsrc_t vr = piece(a.vc, h);
+            if (KL) {
+                __amdgpu_buffer_rsrc_t kr = piece(a.kc, h);
 #pragma unroll
-            for (int i = 0; i < CI; ++i)
-                if (KL) __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, SPAN_LDS(st + TILEB + h * 16 * RB + i * 1024), 16, (int)ksrc[KL ? i : 0], 0, 0, ONCE ? 3 : 0);
+                for (int i = 0; i < CI; ++i)
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, SPAN_LDS(st + TILEB + h * 16 * RB + i * 1024), 16, (int)ksrc[KL ? i : 0], 0, 0, ONCE ? 3 : 0);
+            }
 #pragma unroll
             for (int i = 0; i < CI; ++i)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, SPAN_LDS(st + h * 16 * RB + i * 1024), 16, (int)vsrc[i], 0, 0, ONCE ? 3 : 0);
-#else
-            (void)kr; (void)vr;
-#endif
         }
         if (I16) {  // row scales: lane l takes row l % 32 (the tile's first row where there is none: its weight is 0)
             const int r = lane & 15, h = (lane >> 4) & 1;
             const size_t at = h ? (r < rows[1] ? first[1] + r : first[0]) : (r < rows[0] ? first[0] + r : first[0]);
-#if defined(__HIP_DEVICE_COMPILE__)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a.map.kscale + at), SPAN_LDS(st + SCALES), 4, 0, 0);
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a.map.vscale + at), SPAN_LDS(st + SCALES + 256), 4, 0, 0);
-#else
-            (void)at;
-#endif
         }
+#else
+        (void)st; (void)piece;
+#endif
+    };
+    auto issue_k = [&](int tile) {                // K of the tile that issue_v took last
+        if (KL || tile >= ntiles) return;
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            __amdgpu_buffer_rsrc_t kr = piece(a.kc, h);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kreg[KL ? 0 : h][KL ? 0 : s] = __builtin_amdgcn_raw_buffer_load_b128(kr, c * RB + (4 * s + j) * 16, 0, ONCE ? 3 : 0);
+        }
+#endif
     };
 
-    issue_tile(0, ring);
+    issue_v(0, ring);
+    issue_k(0);
     __builtin_amdgcn_sched_barrier(0);
 
     // ---- Q^T operands: column c of tile nt = query row r0 + TR nt + c % TR; k-step s covers elements 32 s + 8 j + 0..7
@@ -274,7 +285,9 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
 
     auto consume = [&](int tile, unsigned char *st, unsigned char *other) {
         const int key0 = j0 + tile * kSpanTile;
-        if (KL) issue_tile(tile + 1, other);      // into the stage consumed one step ago
+        // V into the stage consumed one step ago: before the scores (79 us against 81 at 32 x 5 tokens over 1030 int16 rows, 32 heads),
+        // but with weights behind them (85.7 against 87.1 at 48 tokens over 2111 rows, 64/8 heads)
+        if (EARLY) issue_v(tile + 1, other);
         __builtin_amdgcn_sched_barrier(0);
         f32x4_t sacc[NT][2];
 #pragma unroll
@@ -304,7 +317,8 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        if (!KL) issue_tile(tile + 1, other);              // K into the registers just used, V into the stage consumed one step ago
+        if (!EARLY) issue_v(tile + 1, other);
+        issue_k(tile + 1);                        // into the registers just used
         __builtin_amdgcn_sched_barrier(0);
         const bool tail = key0 + kSpanTile > nmin || key0 + kSpanTile > j1;  // some query row does not see all of these keys
         if (!I16 && tail) {
