@@ -5,21 +5,34 @@
 //     S^T[32 keys x 16 columns] = K[32 x hd] * Q^T[hd x 16],     O^T[hd x 16 columns] += V^T[hd x 32 keys] * P^T[32 x 16],
 // where q and the probabilities enter the matrix cores as two half terms, with about 22 significant bits, and K and V as stored.  Up to 8
 // query rows share the 16 columns with their low terms (columns c and c + 8: one product for both); with more a column is a row
-// and the low terms take a second product, which leaves the softmax without idle lanes (32 rows of the 32/8-head case: 77 -> XX us).
-// A wavefront takes 8, 16 or 32 query rows; more rows are further workgroups that find the cache rows in the L2 of their XCD.
+// and the low terms take a second product, which leaves the softmax without idle lanes (32 query rows on one wavefront: 77 us as four
+// tiles of 8, 71 as two of 16, at 3 x 8 tokens over 30011 rows, 32/8 heads).
+// A workgroup takes 8, 16 or 32 query rows; more rows are further workgroups that find the cache rows in the L2 of their XCD.
 // A block-scaled int16 n = 64 h + l is taken as h + l / 64: two exact halves by packed 16-bit instructions, five for two elements (h in
-// [-512, 511] and l / 64 in [0, 1) come out of the mantissa of 1024 + x and 16 + x / 64), the factor 64 goes with the row scale.  S^T leaves a lane with 4 keys of a column per 16-key product, which is the
-// layout that P^T needs: key 4 j + i of the first 16 keys is contraction index 8 j + i, of the second 8 j + 4 + i.
+// [-512, 511] and l / 64 in [0, 1) come out of the mantissa of 1024 + x and 16 + x / 64); the factor 64 goes with the row scale.  S^T
+// leaves a lane with 4 keys of a column per 16-key product, which is the layout that P^T needs: key 4 j + i of the first 16 keys is
+// contraction index 8 j + i, of the second 8 j + 4 + i.
 //
 // One pass with a running maximum and sum per query row.  The maximum is raised (and the accumulators rescaled) only when a score
 // exceeds it by more than 2^8, so that most tiles need no reduction across lanes: weights up to 2^8 are as exact in two half terms as
 // weights up to 1.  Scores are kept in units of log 2 (q is scaled by log2(e) / sqrt(hd) before it is split).
 //
-// Memory: each wavefront copies its K and V tiles from HBM into its own LDS ring (buffer loads with the LDS destination, 16 rows per
-// buffer descriptor: pages hold a multiple of 16 rows; rows past the end arrive as zeros), so no barrier is needed in the loop.  16-byte
-// pieces are stored XOR-permuted: K operands (one row per lane) and V operands (transposed by the LDS read) are free of bank conflicts.
-// W = 1, 2 or 4 wavefronts share the rows of a sequence and join through LDS at the end; nsplit workgroups join in a second
-// kernel, which also turns the scores kept in the workspace into weights.
+// Memory: bound by reading K and V once.  Each wavefront copies V tiles from HBM into its own two-stage LDS ring (buffer loads with the
+// LDS destination, 16 rows per buffer descriptor: pages hold a multiple of 16 rows; rows past the end arrive as zeros), so no barrier is
+// needed in the loop.  16-byte pieces are stored XOR-permuted, so that the transposing reads are free of bank conflicts.  K goes straight
+// into the registers that feed the products, which leaves LDS for two workgroups of four wavefronts per compute unit; with 32 query rows,
+// whose registers allow no more than four wavefronts anyway, it goes through the ring as well: whole lines per instruction, and the
+// next tile's copies start before the scores (3 x 8 tokens over 30011 rows: 57 us instead of 69, each at its best number of workgroups).
+// W = 2 or 4 wavefronts share the rows of a sequence and join through LDS at the end; nsplit workgroups join in a second kernel.
+// Weights are added up by the workgroup itself, from the scores it left in the workspace, where it has seen all rows and queries of a kv
+// head, else by the second kernel.
+//
+// Measured, cold caches: 32 x 5 drafts over up to 1030 int16 rows, 32 heads of 128, 79 us (420 MB, 5.3 TB/s); 3 x 8 tokens over up to 30011
+// rows in pages of 64, 32/8 heads, 64 us (308 MB, 4.8 TB/s); 48 tokens with weights over up to 2111 rows, 64/8 heads, 85.5 us (321 MB,
+// 3.8 TB/s: 67 us without the 20 MB of scores that are stored and read again).  A kernel that only reads 300 MB takes 45 us.  A
+// workgroup's first tile arrives 5 to 10 us after the launch (lengths, page numbers and rows depend on each other while every compute
+// unit starts); the loop itself reads 7 TB/s.  Equal shares of all tiles for a fixed number of workgroups instead of whole items
+// balance lengths but leave nothing to overlap a workgroup's start and end with: 95 us for the drafts, 83 with weights.
 #include "kernels.h"
 
 #include <type_traits>
@@ -699,8 +712,11 @@ static int64_t span_items(int B, int T, int Hq, int Hkv) {
 
 int span_attention_splits(int B, int T, int Hq, int Hkv, int hd, int S) {
     const int64_t items = span_items(B, T, Hq, Hkv);
-    int64_t s = items > 0 ? (span_rows(T, Hq / Hkv) == 32 ? 256 : 512) / items : 1;         // two workgroups of four wavefronts per compute unit
-    const int cap = S / 512;                          // each with 512 rows at least at full length
+    // One workgroup of four wavefronts per compute unit: 16 x 4 tokens over 2000 rows (32/8 heads, 128 items) take 26.6 us with 2 splits, 33.7
+    // with 1, 33.9 with 3; 1 x 5 over 2000 int16 rows (32 heads) 16.0 with 8, 36.2 with 1, 17.4 with 16.  Short sequences stay whole: 4 tokens over
+    // 260 rows (32 heads) take 8.2 us on one workgroup per head, 11.6 with 2 splits and the second launch.
+    int64_t s = items > 0 ? 256 / items : 1;
+    const int cap = S / 256;
     if (s > cap) s = cap;
     if (s > 64) s = 64;
     return s < 1 ? 1 : (int)s;
@@ -714,8 +730,10 @@ template <int HD, int RT, bool I16, bool ONCE>
 static void span_launch(const SpanArgs &a, int row_tiles, hipStream_t st) {
     const int items = a.B * a.Hkv * a.nsplit;
     const unsigned blocks = (unsigned)((int64_t)ceil_div(items, 8) * 8 * row_tiles);
-    // wavefronts that share a sequence's rows: four where that does not make more workgroups than run at once (two per compute unit)
-    const bool four = (int64_t)items * row_tiles <= 512;
+    // Wavefronts that share a sequence's rows: four where that does not make more workgroups than run at once, two per compute unit (one
+    // with 32 query rows), else two: 384 items (48 tokens over 2111 rows) 85.7 us with four, 88.7 with two; 4096 (128 x 5 tokens over 390 rows,
+    // 32 heads) 121.6 and 115.4; 512 of 32 query rows (64 x 8 tokens over 1000, 32/8 heads) 46.8 and 42.7.
+    const bool four = (int64_t)items * row_tiles <= (RT == 2 ? 256 : 512);
     if (four && a.weight) span_attention_kernel<HD, RT, 4, I16, ONCE, true><<<blocks, 256, 0, st>>>(a, row_tiles, items);
     else if (four) span_attention_kernel<HD, RT, 4, I16, ONCE, false><<<blocks, 256, 0, st>>>(a, row_tiles, items);
     else if (a.weight) span_attention_kernel<HD, RT, 2, I16, ONCE, true><<<blocks, 128, 0, st>>>(a, row_tiles, items);
