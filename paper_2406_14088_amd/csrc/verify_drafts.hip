@@ -337,6 +337,9 @@ __global__ __launch_bounds__(VD_THREADS) void vd_pick_kernel(VerifyArgs a, int c
     VdWs w;
     vd_ws(a.ws, a.B, T, chunks, &w);
     vd_table(pow2);
+    // the accepted tokens are put out last, by the wavefronts behind the first: their loads travel with the others
+    int at = tid - 64, tok = at >= 0 && at < T ? a.drafts[(size_t)b * T + at] : -1;
+    const float u = greedy ? 0.f : a.u[(size_t)b * (T + 1) + T];
     VdDecision d;
     if (DECIDE) {
         d = vd_decide<VD_THREADS>(a, w, b, chunks, sums, pow2, s_z, s_m, s_arg, &s_stop);
@@ -351,15 +354,25 @@ __global__ __launch_bounds__(VD_THREADS) void vd_pick_kernel(VerifyArgs a, int c
     }
     int32_t *tokens = a.tokens + (size_t)b * (T + 1);
     float *logp = a.logp ? a.logp + (size_t)b * (T + 1) : nullptr;
-    auto put = [&](int i, int tok) {
+    auto put = [&](int i, int tok, float x) {     // x: the token's logit
         tokens[i] = tok;
-        if (logp) logp[i] = tok < 0 ? 0.f : (float)(((double)vd_row(a, b, i)[tok] - (double)s_m[i]) * (greedy ? 1.0 : 1.0 / a.temperature) - log(s_z[i]));
+        if (logp) logp[i] = tok < 0 ? 0.f : (float)(((double)x - (double)s_m[i]) * (greedy ? 1.0 : 1.0 / a.temperature) - log(s_z[i]));
     };
+    auto logit = [&](int i, int tok) { return logp && tok >= 0 ? vd_row(a, b, i)[tok] : 0.f; };
+    if (at >= d.stop) tok = -1;
+    const float x_tok = at >= 0 ? logit(at, tok) : 0.f;
     if (tid == 0) a.accepted[b] = d.stop;
-    for (int i = tid; i <= T; i += VD_THREADS)
-        if (i != d.stop) put(i, i < d.stop ? a.drafts[(size_t)b * T + i] : -1);
+    auto put_others = [&] {
+        if (at >= 0 && at <= T && at != d.stop) put(at, tok, x_tok);
+        for (int i = at + VD_THREADS - 64; at >= 0 && i <= T; i += VD_THREADS - 64) {
+            const int t = i < d.stop ? a.drafts[(size_t)b * T + i] : -1;
+            if (i != d.stop) put(i, t, logit(i, t));
+        }
+    };
     if (d.bad || greedy) {
-        if (tid == 0) put(d.stop, d.bad ? -1 : s_arg[d.stop]);
+        const int next = d.bad ? -1 : s_arg[d.stop];
+        if (tid == 0) put(d.stop, next, logit(d.stop, next));
+        put_others();
         return;
     }
 
@@ -406,21 +419,22 @@ __global__ __launch_bounds__(VD_THREADS) void vd_pick_kernel(VerifyArgs a, int c
         const float cm = w.max[cell + k];
         return cm == -INFINITY ? 0.0 : w.sum[cell + k] * vd_weight(cm, mp, c, pow2) * ip;
     };
-    double total = 0.0;
+    double total, v0;                             // v0: of the first 64 chunks, kept
     for (;;) {
-        total = 0.0;
-        for (int k0 = 0; k0 < chunks; k0 += 64) total += vd_wave_sum(k0 + lane < chunks ? mass(k0 + lane) : 0.0);
+        v0 = lane < chunks ? mass(lane) : 0.0;
+        total = vd_wave_sum(v0);
+        for (int k0 = 64; k0 < chunks; k0 += 64) total += vd_wave_sum(k0 + lane < chunks ? mass(k0 + lane) : 0.0);
         if (!residual || total > 0.0) break;
         residual = false;  // p and q are the same: p itself
     }
-    const double target = (double)a.u[(size_t)b * (T + 1) + T] * total;
+    const double target = (double)u * total;
     // the chunk that the draw falls into: the first whose running sum exceeds it (the last with weight, should none by rounding)
     int chosen = 0;
     double before = 0.0;
     {
         double run = 0.0;
         for (int k0 = 0; k0 < chunks; k0 += 64) {
-            const double v = k0 + lane < chunks ? mass(k0 + lane) : 0.0;
+            const double v = k0 == 0 ? v0 : k0 + lane < chunks ? mass(k0 + lane) : 0.0;
             double incl = v;
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {
@@ -484,8 +498,9 @@ __global__ __launch_bounds__(VD_THREADS) void vd_pick_kernel(VerifyArgs a, int c
         for (int k = 3; k >= 0; --k)
             if (s_first[k] >= 0) next = s_first[k];
         for (int k = 3; k >= 0 && next < 0; --k) next = s_last[k];  // by rounding nobody's: the last token with weight
-        put(d.stop, next);
+        put(d.stop, next, logit(d.stop, next));
     }
+    put_others();
 }
 
 // Logits per wavefront: 2048 where that still gives every compute unit a dozen wavefronts, else 512.
