@@ -5,6 +5,9 @@
 // elements of a head -- four pairs, or 8 neighbours of the part that does not rotate -- as two 16-byte loads per partial, issued before the
 // positions are known, so that the chain of latencies is positions -> table -> stores.  8 or 16 consecutive lanes hold a head: the
 // maximum of a block-scaled row is a reduction among them.
+//
+// Measured: 8 x 509 tokens, 32/8 heads of 128, paged, 40 us (185 MB, 4.6 TB/s; a copy of 4 GiB reaches 4.8); 32 x 5 tokens, 32 heads, four
+// partials, 7.8 us (37 MB, 4.7 TB/s).
 #include "kernels.h"
 
 template <bool SCALED>

@@ -8,7 +8,11 @@
 // relative error e move a draw to a neighbour with a probability of the order of V * e, about one in a hundred for fp32 (1e-7) and
 // V = 128256.  So weights and sums are fp64: 2^g from a table of 128 powers in LDS and a polynomial of degree 3 for the rest
 // (interpolation at the Chebyshev nodes, relative error 6e-13), 11 fp64 instructions per logit.  They take twice the time of fp32 ones and
-// bound the reading of the rows (with a polynomial of degree 8 and no table, 15 of them).
+// bound the reading of the rows (with a polynomial of degree 8 and no table, 15 of them): 4.7 TB/s, 6.3 TB/s for the maxima alone.
+//
+// Measured: 64 x 5 drafts, vocabulary 32000 (90 MB): 43 us, of it 22 for the rows, 5 for the decision, 7 for the weights of the rejected row
+// and 8 for the token, the last three a chain of dependent loads each; 128 x up to 7 drafts, vocabulary 128256: 145 us (rows 108, 9, 25, 10).
+// One workgroup per sequence that decides and picks, without the kernels between, took 2.5 times as long for the second.
 #include "kernels.h"
 
 #define VD_THREADS 256
@@ -103,8 +107,8 @@ __device__ __forceinline__ const float *vd_row(const VerifyArgs &a, int b, int r
     return r <= a.T ? a.target + ((size_t)b * (a.T + 1) + r) * a.ldt : a.draft + ((size_t)b * a.T + (r - a.T - 1)) * a.ldd;
 }
 
-// One wavefront per (row, chunk of 64 * EPT logits), four chunks of a row per workgroup: the logits stay in registers between the maximum and the weights, which refer to the
-// chunk's own maximum.  SUMS, ARG: whether the sum and the index of the maximum are wanted (sampled: sums; greedy: the index, and sums for
+// One wavefront per (row, chunk of 64 * EPT logits), four chunks of a row per workgroup: the logits stay in registers between the maximum
+// and the weights, which refer to the chunk's own maximum.  SUMS, ARG: whether the sum and the index of the maximum are wanted (sampled: sums; greedy: the index, and sums for
 // log-probabilities).
 template <int EPT, bool SUMS, bool ARG>
 __global__ __launch_bounds__(VD_THREADS, 8) void vd_rows_kernel(VerifyArgs a, int chunks, int rows, int groups) {
@@ -503,8 +507,12 @@ __global__ __launch_bounds__(VD_THREADS) void vd_pick_kernel(VerifyArgs a, int c
     put_others();
 }
 
-// Logits per wavefront: 2048 where that still gives every compute unit a dozen wavefronts, else 512.
-static int vd_chunk_len(int B, int T, int V) { return (int64_t)B * (T + 1) * ceil_div(V, 2048) >= 2048 ? 2048 : 512; }
+// Logits per wavefront: 512 where 2048 would leave a compute unit less than four wavefronts and a sequence has few chunks to join, else
+// 2048.  With 512 and 2048: 1 x 3 drafts, vocabulary 1024: 17.1 and 19.3 us; 8 x 5, 32000: 23.6 and 24.3; 16 x 5, 32000: 27.4 and 26.5; 64 x 5, 32000:
+// 50.8 and 43.2; and where a workgroup joins more than 512 chunks: 2 x 16, 32000: 30.8 and 26.8; 1 x 4, 128256: 31.6 and 22.9.
+static int vd_chunk_len(int B, int T, int V) {
+    return (int64_t)B * (T + 1) * ceil_div(V, 2048) < 1024 && (int64_t)(T + 1) * ceil_div(V, 512) <= 512 ? 512 : 2048;
+}
 
 size_t verify_drafts_ws_bytes(int B, int T, int V) { return vd_ws(nullptr, B, T, ceil_div(V, vd_chunk_len(B, T, V)), nullptr) + 8; }
 
