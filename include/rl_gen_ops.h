@@ -283,7 +283,8 @@ size_t rl_op_span_attention_ws_floats(int32_t B, int32_t T, int32_t Hq, int32_t 
  * already lie below slot `keep` are not touched, and the j-th free slot below `keep` (ascending) receives the j-th staying row at or
  * above it (ascending): K and V rows and their scales, in place.  weight_out / pos_out: the values of the rows now in slots
  * 0 .. min(n, keep) - 1, entries behind are left as they were; each may be the array it is taken from (pos_out is required with pos).
- * d_len_out (DEVICE int32 [B], may be d_len, or NULL): min(n, keep).  1 <= keep <= S, 0 <= recent <= keep.
+ * d_len_out (DEVICE int32 [B], may be d_len, or NULL): min(n, keep).  1 <= keep <= S, 0 <= recent <= keep.  Page lists of different
+ * sequences must not share pages with rows that move or are moved onto.
  * ws: DEVICE, ws_bytes long, 8-byte aligned, at least rl_op_evict_rows_ws_bytes (else RL_GEN_E_CAPACITY). */
 int rl_op_evict_rows(uint16_t *kc, uint16_t *vc, float *kscale, float *vscale, const int32_t *table, int32_t table_stride,
                      int32_t page_size, const float *weight, float *weight_out, const int32_t *pos, int32_t *pos_out, const int32_t *d_len,
@@ -305,7 +306,8 @@ size_t rl_op_evict_rows_ws_bytes(int32_t B, int32_t Hkv, int32_t S, int32_t keep
  * reached and holds a NaN (temperature > 0: or no finite largest value) ends the sequence's acceptance, and its next token is -1.
  * logp fp32 [B, T+1] or NULL: log p of each token of `tokens` under the target row it follows (temperature <= 0: at temperature 1, and
  * NaN where that row's largest logit is not finite), 0 for -1.
- * Weights and sums are formed in fp64 from the fp32 logits (relative error below 1e-11), in a fixed order.  1 <= T <= 256.
+ * Weights and sums are formed in fp64 from the fp32 logits (relative error below 1e-11), in a fixed order.  1 <= T <= 256,
+ * 1 <= V <= 2^30.
  * ws: DEVICE, ws_bytes long, 8-byte aligned, at least rl_op_verify_drafts_ws_bytes (else RL_GEN_E_CAPACITY). */
 int rl_op_verify_drafts(const float *target, int64_t ldt, const float *draft, int64_t ldd, const int32_t *drafts, const float *u,
                         const int32_t *d_span, int32_t B, int32_t T, int32_t V, double temperature, int32_t *accepted, int32_t *tokens,

@@ -1823,7 +1823,7 @@ int rl_op_evict_rows(uint16_t *kc, uint16_t *vc, float *kscale, float *vscale, c
 }
 
 static bool verify_shape_ok(int32_t B, int32_t T, int32_t V) {
-    return B >= 0 && T >= 1 && T <= 256 && V > 0 && (int64_t)B * (2 * (int64_t)T + 1) * ((V + (int64_t)511) / 512) <= INT32_MAX;
+    return B >= 0 && T >= 1 && T <= 256 && V > 0 && V <= 1 << 30 && (int64_t)B * (2 * (int64_t)T + 1) * ((V + (int64_t)511) / 512) <= INT32_MAX;
 }
 
 size_t rl_op_verify_drafts_ws_bytes(int32_t B, int32_t T, int32_t V) { return verify_shape_ok(B, T, V) ? verify_drafts_ws_bytes(B, T, V) : 0; }

@@ -75,6 +75,8 @@ def test_sizes_and_options(L):
     for kw in (dict(T=0), dict(T=257), dict(V=0), dict(ldt=99), dict(d=P, ldd=99), dict(temp=float("nan")), dict(temp=float("inf")), dict(temp=1e-40),
                dict(B=-1), dict(B=1 << 30), dict(ws=P + 4)):
         assert _verify(L, **kw) == E_SHAPE, kw
+    assert _verify(L, B=1, T=1, V=(1 << 30) + 1, ldt=1 << 31, wsn=1 << 40) == E_SHAPE  # behind it a chunk's first index would pass 31 bits
+    assert L.rl_op_verify_drafts_ws_bytes(1, 1, (1 << 30) + 1) == 0 < L.rl_op_verify_drafts_ws_bytes(1, 1, 1 << 30)
     assert _verify(L, temp=0.0, u=None, ws=None) == E_NULL
 
 
