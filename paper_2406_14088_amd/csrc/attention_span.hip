@@ -24,12 +24,13 @@
 // whose registers allow no more than four wavefronts anyway, it goes through the ring as well: whole lines per instruction, and the
 // next tile's copies start before the scores (3 x 8 tokens over 30011 rows: 57 us instead of 69, each at its best number of workgroups).
 // W = 2 or 4 wavefronts share the rows of a sequence and join through LDS at the end; nsplit workgroups join in a second kernel.
-// Weights are added up by the workgroup itself, from the scores it left in the workspace, where it has seen all rows and queries of a kv
-// head, else by the second kernel.
+// Weights need the scores again once maximum and sum are final.  A workgroup with up to 16 query rows that has seen all rows and queries
+// of a kv head keeps them lane by lane, most of them in registers, and adds up the weights itself; else they go to the workspace and the
+// second kernel does.
 //
 // Measured, cold caches: 32 x 5 drafts over up to 1030 int16 rows, 32 heads of 128, 79 us (420 MB, 5.3 TB/s); 3 x 8 tokens over up to 30011
-// rows in pages of 64, 32/8 heads, 64 us (308 MB, 4.8 TB/s); 48 tokens with weights over up to 2111 rows, 64/8 heads, 85.5 us (321 MB,
-// 3.8 TB/s: 67 us without the 20 MB of scores that are stored and read again).  A kernel that only reads 300 MB takes 45 us.  A
+// rows in pages of 64, 32/8 heads, 64 us (308 MB, 4.8 TB/s); 48 tokens with weights over up to 2111 rows, 64/8 heads, 77.6 us (321 MB,
+// 4.1 TB/s; 86 with all scores in the workspace, 67 without weights).  A kernel that only reads 300 MB takes 45 us.  A
 // workgroup's first tile arrives 5 to 10 us after the launch (lengths, page numbers and rows depend on each other while every compute
 // unit starts); the loop itself reads 7 TB/s.  Equal shares of all tiles for a fixed number of workgroups instead of whole items
 // balance lengths but leave nothing to overlap a workgroup's start and end with: 95 us for the drafts, 83 with weights.
@@ -46,6 +47,11 @@ static constexpr float kSpanSlack = 8.f;    // how far (in powers of two) a weig
 
 __device__ __forceinline__ float span_ror8(float v) {  // lane l of a row of 16 receives lane (l + 8) % 16
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xf, 0xf, true));
+}
+// Another lane of the row of 16: 0xb1: lane ^ 1, 0x4e: lane ^ 2, 0x141 / 0x140: mirrored half row / row.
+template <int CTRL>
+__device__ __forceinline__ float span_dpp(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
 __device__ __forceinline__ float span_max_groups(float v) {  // over the four lane groups that hold one column
     v = fmaxf(v, __shfl_xor(v, 16, 64));
@@ -97,14 +103,17 @@ __device__ __forceinline__ void span_extent(const SpanArgs &a, int b, int *n0, i
 
 // ONCE: no other workgroup reads these cache rows (one row tile), so their copies are non-temporal: they stream faster.
 // RT: 0: 8 query rows with both terms in one tile; 1, 2: so many tiles of 16 rows.
-// WT: the scores are kept and the weights added up.
-template <int HD, int RT, int W, bool I16, bool ONCE, bool WT>
+// WT: 0: no weights.  1: the scores go to the workspace, the second kernel adds the weights up.  2: this workgroup sees all rows and
+// queries of a kv head and adds them up itself, from scores that every lane kept: the first KEEP tiles' in registers, further ones in the
+// workspace.
+template <int HD, int RT, int W, bool I16, bool ONCE, int WT>
 __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel(SpanArgs a, int row_tiles, int items) {
     constexpr int RB = HD * 2;                    // bytes of a cache row
     constexpr int KS = HD / 32, OT = HD / 16;     // k-steps of a score, tiles of the output
     constexpr int TILEB = kSpanTile * RB;
     constexpr bool KL = RT == 2;                  // K through LDS as well
     constexpr bool EARLY = KL || !WT;
+    constexpr int NV = RT ? 8 : 4, KEEP = WT == 2 ? (RT ? 8 : 16) : 0;  // scores of a lane per tile and column tile
     constexpr int SCALES = KL ? 2 * TILEB : TILEB, STAGE = SCALES + (I16 ? 512 : 0);  // a V tile, with KL a K tile, the row scales of K and V
     constexpr int LPR = RB / 16;                  // lanes per row of a copy instruction
     constexpr int NT = RT ? RT : 1, TR = RT ? 16 : 8, ROWS = TR * NT;  // column tiles, query rows of a tile and of this workgroup
@@ -296,6 +305,13 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
     const size_t row_base = ((size_t)b * a.Hkv + kvh) * a.T * G;  // query rows in the workspace: [b][kv head][t * G + g]
     float *scores = a.ws + w.scores + ((size_t)b * a.Hkv + kvh) * w.slab + (size_t)rt * w.tiles * (ROWS * kSpanTile);
 
+    float kept[KEEP ? KEEP : 1][NT][NV];          // scores of the first tiles
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < NV; ++e) kept[i][nt][e] = 0.f;
     auto consume = [&](int tile, unsigned char *st, unsigned char *other) {
         const int key0 = j0 + tile * kSpanTile;
         // V into the stage consumed one step ago: before the scores (79 us against 81 at 32 x 5 tokens over 1030 int16 rows, 32 heads),
@@ -390,7 +406,15 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
                 for (int e = 0; e < 8; ++e)
                     if (key0 + 16 * (e >> 2) + 4 * j + (e & 3) >= (lim[nt] < j1 ? lim[nt] : j1)) v[e] = -INFINITY;
             }
-            if (WT) {                             // lanes of the low term store the second 16 keys
+            if (WT == 2) {
+#pragma unroll
+                for (int e = 0; e < NV; ++e) {
+                    const float x = RT || c < 8 ? v[e] : v[4 + (e & 3)];
+#pragma unroll
+                    for (int i = 0; i < KEEP; ++i) kept[i][nt][e] = tile == i ? x : kept[i][nt][e];  // (a branch here becomes an index into scratch)
+                }
+            }
+            if (WT && tile >= KEEP) {             // lanes of the low term take the second 16 keys
                 float *sp = scores + (size_t)(key0 / kSpanTile) * (ROWS * kSpanTile) + (TR * nt + c % TR) * kSpanTile + 4 * j;
                 if (RT) {
                     *reinterpret_cast<f32x4_t *>(sp) = f32x4_t{v[0], v[1], v[2], v[3]};
@@ -487,7 +511,7 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
         unsigned char *st = ring + (tile & 1) * STAGE;
         __builtin_amdgcn_sched_barrier(0);
         // the tile has landed once nothing older than those stores is pending: vmcnt(0) or (STORES) only
-        if (tile == 0 || !WT) __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));
+        if (tile <= KEEP || !WT) __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));
         else __builtin_amdgcn_s_waitcnt(STORES | (7 << 4) | (15 << 8));
         __builtin_amdgcn_sched_barrier(0);
         consume(tile, st, ring + (~tile & 1) * STAGE);
@@ -516,7 +540,6 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
     }
     __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));  // the score stores have arrived
     __syncthreads();
-    const bool weigh = ONCE && WT && a.nsplit == 1;  // this workgroup has seen all queries and rows of its kv head
     constexpr int TPR = HD / 8;                     // threads per query row, 8 elements each
     for (int r = threadIdx.x / TPR; r < ROWS && r0 + r <= rlast; r += 64 * W / TPR) {
         const int e0 = (threadIdx.x % TPR) * 8;
@@ -535,7 +558,7 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
         }
         const int rr = r0 + r;
         const size_t row = row_base + rr;
-        if (weigh) {
+        if (WT == 2) {
             if (e0 == 0) { s_rows[0][r] = m; s_rows[1][r] = 1.0f / d; }
         } else if (a.nsplit > 1 || WT) {
             if (e0 == 0) {
@@ -560,46 +583,65 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
             if (a.out_lo) *reinterpret_cast<u32x4_t *>(a.out_lo + at) = l;
         }
     }
-    if (weigh) {
+    if (WT == 2) {
         __syncthreads();
         float *wt = a.weight + ((size_t)b * a.Hkv + kvh) * a.S;
-        constexpr int STEP = 256 * W;
-        auto pass = [&](auto two, int key) {      // 4 keys of a thread, or 4 and 4 a step apart: all loads of 8 query rows in flight
-            constexpr int P = decltype(two)::value ? 2 : 1;
-            float sum[P][4], old[P][4];
+        float m[NT], inv[NT];
 #pragma unroll
-            for (int p = 0; p < P; ++p)
+        for (int nt = 0; nt < NT; ++nt) { m[nt] = s_rows[0][TR * nt + c % TR]; inv[nt] = s_rows[1][TR * nt + c % TR]; }
+        // Sums over the query rows, which are lanes of a group of 8 or 16; 4 keys of a tile are put out by one lane of it (two with RT).
+        const bool puts = RT ? c < 2 : c % 8 == 0;
+        const int half = RT ? c & 1 : c >> 3;
+        auto weigh = [&](int t0, auto score) {    // 8 tiles: what was there travels meanwhile
+            float old[8][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) { sum[p][i] = 0.f; old[p][i] = key + p * STEP + i < nmax ? wt[key + p * STEP + i] : 0.f; }
-            for (int rb = 0; rb <= rlast; rb += 8) {
-                f32x4_t x[P][8];
+            for (int u = 0; u < 8; ++u)
 #pragma unroll
-                for (int p = 0; p < P; ++p)
+                for (int e = 0; e < 4; ++e) {
+                    const int key = j0 + (t0 + u) * kSpanTile + 16 * half + 4 * j + e;
+                    old[u][e] = puts && key < j1 ? wt[key] : 0.f;
+                }
 #pragma unroll
-                    for (int r = 0; r < 8; ++r) {  // rows behind the last one are part of the block
-                        const int k = key + p * STEP;
-                        x[p][r] = k < nmax ? *reinterpret_cast<const f32x4_t *>(scores + (size_t)(k / kSpanTile) * (ROWS * kSpanTile) + (rb + r) * kSpanTile + k % kSpanTile) : f32x4_t{0.f, 0.f, 0.f, 0.f};
-                    }
+            for (int u = 0; u < 8; ++u) {
+                if (t0 + u >= ntiles) break;
+                const int key0 = j0 + (t0 + u) * kSpanTile + 4 * j;
+                float sum[NV];
 #pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    if (rb + r > rlast) break;
-                    const int last = limit(rb + r);
-                    const float m = s_rows[0][rb + r], inv = s_rows[1][rb + r];
+                for (int e = 0; e < NV; ++e) {
+                    const int key = key0 + (RT ? 16 * (e >> 2) + (e & 3) : 16 * half + e);
+                    sum[e] = 0.f;
 #pragma unroll
-                    for (int p = 0; p < P; ++p)
+                    for (int nt = 0; nt < NT; ++nt) sum[e] += row_ok[nt] && key < lim[nt] ? __builtin_amdgcn_exp2f(score(u, nt, e) - m[nt]) * inv[nt] : 0.f;
+                    sum[e] += span_dpp<0xb1>(sum[e]);       // lanes c ^ 1, c ^ 2, then the mirrored half row and row
+                    sum[e] += span_dpp<0x4e>(sum[e]);
+                    sum[e] += span_dpp<0x141>(sum[e]);
+                    if (RT) sum[e] += span_dpp<0x140>(sum[e]);
+                }
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) sum[p][i] += key + p * STEP + i < last ? __builtin_amdgcn_exp2f(x[p][r][i] - m) * inv : 0.f;
+                for (int e = 0; e < 4; ++e) {
+                    const int key = key0 + 16 * half + e;
+                    if (puts && key < j1) wt[key] = old[u][e] + (RT && half ? sum[NV - 4 + e] : sum[e]);
                 }
             }
-#pragma unroll
-            for (int p = 0; p < P; ++p)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (key + p * STEP + i < nmax) wt[key + p * STEP + i] = old[p][i] + sum[p][i];
         };
-        int key = threadIdx.x * 4, left = nmax;   // the last threads' keys of a pass decide how many steps it takes
-        for (; left > STEP; left -= 2 * STEP, key += 2 * STEP) pass(std::true_type(), key);
-        if (left > 0) pass(std::false_type(), key);
+#pragma unroll
+        for (int t0 = 0; t0 < KEEP; t0 += 8)
+            if (t0 < ntiles) weigh(t0, [&](int u, int nt, int e) { return kept[t0 + u][nt][e]; });
+        for (int t0 = KEEP; t0 < ntiles; t0 += 8) {
+            float x[8][NT][NV];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int q = 0; q < NV / 4; ++q) {
+                        const float *sp = scores + (size_t)(j0 / kSpanTile + t0 + u) * (ROWS * kSpanTile) + (TR * nt + c % TR) * kSpanTile + 4 * j;
+                        const f32x4_t y = t0 + u < ntiles ? *reinterpret_cast<const f32x4_t *>(sp + 16 * (RT ? q : half)) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[u][nt][4 * q + e] = y[e];
+                    }
+            weigh(t0, [&](int u, int nt, int e) { return x[u][nt][e]; });
+        }
     }
 }
 
@@ -734,10 +776,16 @@ static void span_launch(const SpanArgs &a, int row_tiles, hipStream_t st) {
     // with 32 query rows), else two: 384 items (48 tokens over 2111 rows) 85.7 us with four, 88.7 with two; 4096 (128 x 5 tokens over 390 rows,
     // 32 heads) 121.6 and 115.4; 512 of 32 query rows (64 x 8 tokens over 1000, 32/8 heads) 46.8 and 42.7.
     const bool four = (int64_t)items * row_tiles <= (RT == 2 ? 256 : 512);
-    if (four && a.weight) span_attention_kernel<HD, RT, 4, I16, ONCE, true><<<blocks, 256, 0, st>>>(a, row_tiles, items);
-    else if (four) span_attention_kernel<HD, RT, 4, I16, ONCE, false><<<blocks, 256, 0, st>>>(a, row_tiles, items);
-    else if (a.weight) span_attention_kernel<HD, RT, 2, I16, ONCE, true><<<blocks, 128, 0, st>>>(a, row_tiles, items);
-    else span_attention_kernel<HD, RT, 2, I16, ONCE, false><<<blocks, 128, 0, st>>>(a, row_tiles, items);
+    auto launch = [&](auto wt) {
+        constexpr int WT = decltype(wt)::value;
+        if (four) span_attention_kernel<HD, RT, 4, I16, ONCE, WT><<<blocks, 256, 0, st>>>(a, row_tiles, items);
+        else span_attention_kernel<HD, RT, 2, I16, ONCE, WT><<<blocks, 128, 0, st>>>(a, row_tiles, items);
+    };
+    // Weights by the workgroup itself (WT 2) and by the second kernel (WT 1), 64/8 heads over up to 2111 rows: 48 x 1 tokens 78 us and 86, 48 x 2 (16
+    // query rows) 99.5 and 105, 48 x 4 (32 query rows, whose lanes keep 16 scores a tile and add over 16 lanes) 133 and 117.
+    if (!a.weight) launch(std::integral_constant<int, 0>());
+    else if (RT < 2 && a.nsplit == 1) launch(std::integral_constant<int, RT < 2 ? 2 : 1>());
+    else launch(std::integral_constant<int, 1>());
 }
 template <int HD, bool I16>
 static void span_launch_tiles(const SpanArgs &a, hipStream_t st) {
@@ -753,7 +801,7 @@ void launch_span_attention(const SpanArgs &a, hipStream_t st) {
     if (a.hd == 128) a.map.kscale ? span_launch_tiles<128, true>(a, st) : span_launch_tiles<128, false>(a, st);
     else a.map.kscale ? span_launch_tiles<64, true>(a, st) : span_launch_tiles<64, false>(a, st);
     const int merge_blocks = a.nsplit > 1 ? (int)(((int64_t)a.B * a.T * a.Hq + 3) / 4) : 0;
-    const bool several = a.nsplit > 1 || (int64_t)a.T * (a.Hq / a.Hkv) > 32;
+    const bool several = a.nsplit > 1 || span_rows(a.T, a.Hq / a.Hkv) > 16;
     const int key_blocks = a.weight && several ? ceil_div(a.S, 1024) : 0;
     const int64_t blocks = merge_blocks + (int64_t)a.B * a.Hkv * key_blocks;
     if (blocks > 0) (a.hd == 128 ? span_join_kernel<128> : span_join_kernel<64>)<<<(unsigned)blocks, 256, 0, st>>>(a, merge_blocks, key_blocks ? key_blocks : 1);

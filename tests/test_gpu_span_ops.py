@@ -124,6 +124,25 @@ def test_span_attention_splits_join(nsplit, block_scaled):
     _check_span(cache, _rnd(g, B, T, Hq, hd, std=2.0), [250, 0, 100], T, nsplit)
 
 
+@pytest.mark.parametrize("T,Hq,hd", [(1, 16, 128), (2, 10, 64), (2, 16, 128), (4, 8, 64)])
+@pytest.mark.parametrize("block_scaled", [False, True])
+def test_span_attention_weights_of_long_unsplit_sequences(T, Hq, hd, block_scaled):
+    # scores of 8 (up to 8 query rows: 16) tiles of 32 rows stay in a wavefront's registers, four wavefronts share a sequence: either side of 2048 and 1024 rows
+    lens = [2600, 2048 - T, 2048, 1024 - T, 1025, 1]
+    B, Hkv, S = len(lens), 2, 2608
+    g = torch.Generator().manual_seed(T * hd + Hq)
+    cache = R.Cache(_rnd(g, B, Hkv, S, hd), _rnd(g, B, Hkv, S, hd), block_scaled)
+    _check_span(cache, _rnd(g, B, T, Hq, hd, std=1.5), lens, T, 1)
+
+
+@pytest.mark.parametrize("T,Hq", [(1, 64), (2, 64), (4, 64), (5, 64)])
+def test_span_attention_weights_of_many_sequences(T, Hq):
+    B, Hkv, hd, S = 65, 8, 64, 96                      # more kv heads than workgroups of four wavefronts run at once
+    g = torch.Generator().manual_seed(T)
+    cache = R.Cache(_rnd(g, B, Hkv, S, hd), _rnd(g, B, Hkv, S, hd), False)
+    _check_span(cache, _rnd(g, B, T, Hq, hd), torch.randint(0, S - T + 1, (B,), generator=g).tolist(), T)
+
+
 @pytest.mark.parametrize("page", [0, 64])
 def test_span_attention_of_ragged_spans(page):
     B, T, Hq, Hkv, hd, S = 5, 6, 8, 2, 128, 128
