@@ -243,7 +243,7 @@ struct VerifyArgs {
     const float *u;
     const int32_t *d_span;
     int B, T, V;
-    double temperature;
+    double temperature, rate, least;  // the last two set by the launcher
     int32_t *accepted, *tokens;
     float *logp;
     void *ws;

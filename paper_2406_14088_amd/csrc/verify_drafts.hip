@@ -55,7 +55,8 @@ __device__ __forceinline__ void vd_table(double *pow2) {
 static constexpr double kVdLog2e = 1.4426950408889634074 * 128;  // exponents are counted in 128ths
 static constexpr double kVdLeast = -1020.0 * 128;                // weights below 2^-1020 of the largest count as zero
 
-// 2^(d c / 128) for kVdLeast <= d c <= 128000 (c = kVdLog2e / temperature).
+// 2^(d c / 128) for kVdLeast <= d c <= 128000 (c = kVdLog2e / temperature: VerifyArgs::rate, from the host, since two fp64 divisions cost a
+// wavefront as much as eight logits).
 __device__ __forceinline__ double vd_exp(double d, double c, const double *pow2) {
     const double magic = 6755399441055744.0;  // 1.5 * 2^52: adding it leaves the nearest integer in the low bits
     const double t = __builtin_fma(d, c, magic);
@@ -67,12 +68,11 @@ __device__ __forceinline__ double vd_exp(double d, double c, const double *pow2)
     return __builtin_fma(s, q, s);
 }
 // The weight of a logit x next to the largest one m; 0 for x = -inf.
-__device__ __forceinline__ double vd_weight(float x, double m, double c, const double *pow2) {
-    const double d = (double)x - m, least = kVdLeast / c;
-    const double w = vd_exp(__builtin_fmax(d, least), c, pow2);
-    return d >= least ? w : 0.0;
+__device__ __forceinline__ double vd_weight(float x, double m, const VerifyArgs &a, const double *pow2) {
+    const double d = (double)x - m;
+    const double w = vd_exp(__builtin_fmax(d, a.least), a.rate, pow2);
+    return d >= a.least ? w : 0.0;
 }
-__device__ __forceinline__ double vd_rate(const VerifyArgs &a) { return kVdLog2e / (a.temperature > 0 ? a.temperature : 1.0); }
 
 // Workspace: per (sequence, row, chunk) sum, maximum and index of the maximum (-1: the chunk holds a NaN); per sequence and target
 // row its maximum and sum; per (sequence, chunk) the weight of the decisive row; per sequence what was decided.
@@ -168,13 +168,12 @@ __global__ __launch_bounds__(VD_THREADS, 8) void vd_rows_kernel(VerifyArgs a, in
     }
     double s = 0.0;
     if (SUMS) {
-        const double md = m == -INFINITY ? 0.0 : (double)m, c = vd_rate(a);
-        const double least = kVdLeast / c;
+        const double md = m == -INFINITY ? 0.0 : (double)m;
         double s1 = 0.0;
 #pragma unroll
         for (int e = 0; e < EPT; e += 2) {
-            s += vd_exp(__builtin_fmax((double)x[e] - md, least), c, pow2);
-            s1 += vd_exp(__builtin_fmax((double)x[e + 1] - md, least), c, pow2);
+            s += vd_exp(__builtin_fmax((double)x[e] - md, a.least), a.rate, pow2);
+            s1 += vd_exp(__builtin_fmax((double)x[e + 1] - md, a.least), a.rate, pow2);
         }
         s = vd_wave_sum(s + s1);
     }
@@ -196,7 +195,6 @@ __device__ VdDecision vd_decide(const VerifyArgs &a, const VdWs &w, int b, int c
                                 int *s_stop) {
     const int n = vd_span(a, b), T = a.T, tid = threadIdx.x;
     const bool greedy = !(a.temperature > 0);
-    const double c = vd_rate(a);
     const int rows = a.draft ? 2 * T + 1 : T + 1;
     if (tid == 0) *s_stop = n;
     __syncthreads();  // the table as well
@@ -237,7 +235,7 @@ __device__ VdDecision vd_decide(const VerifyArgs &a, const VdWs &w, int b, int c
 #pragma unroll 4
             for (int k = l; k < chunks; k += 16) {
                 const float cm = w.max[cell + k];
-                z += cm == -INFINITY ? 0.0 : w.sum[cell + k] * vd_weight(cm, m, c, pow2);
+                z += cm == -INFINITY ? 0.0 : w.sum[cell + k] * vd_weight(cm, m, a, pow2);
             }
 #pragma unroll
             for (int o = 8; o > 0; o >>= 1) z += __shfl_xor(z, o, 64);
@@ -256,9 +254,9 @@ __device__ VdDecision vd_decide(const VerifyArgs &a, const VdWs &w, int b, int c
             if (a.draft) {
                 const int r = T + 1 + i;
                 go = s_arg[r] >= 0;
-                if (go) q = vd_weight(xq, s_m[r], c, pow2) / s_z[r];
+                if (go) q = vd_weight(xq, s_m[r], a, pow2) / s_z[r];
             }
-            go = go && in && (double)u * q < vd_weight(xp, s_m[i], c, pow2) / s_z[i];
+            go = go && in && (double)u * q < vd_weight(xp, s_m[i], a, pow2) / s_z[i];
         }
         if (!go) atomicMin(s_stop, i);
     }
@@ -313,12 +311,12 @@ __global__ __launch_bounds__(VD_THREADS) void vd_residual_kernel(VerifyArgs a, i
         y[k] = qrow[v];
     }
     const size_t row0 = (size_t)b * (2 * a.T + 1);
-    const double c = vd_rate(a), mp = w.row_max[row0 + rp], mq = w.row_max[row0 + rq], ip = 1.0 / w.row_sum[row0 + rp], iq = 1.0 / w.row_sum[row0 + rq];
+    const double mp = w.row_max[row0 + rp], mq = w.row_max[row0 + rq], ip = 1.0 / w.row_sum[row0 + rp], iq = 1.0 / w.row_sum[row0 + rq];
     __syncthreads();
     double s = 0.0;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        const double e = vd_weight(x[k], mp, c, pow2) * ip - vd_weight(y[k], mq, c, pow2) * iq;
+        const double e = vd_weight(x[k], mp, a, pow2) * ip - vd_weight(y[k], mq, a, pow2) * iq;
         s += e > 0.0 && first + tid + k * VD_THREADS < last ? e : 0.0;
     }
     s = vd_wave_sum(s);
@@ -337,7 +335,6 @@ __global__ __launch_bounds__(VD_THREADS) void vd_pick_kernel(VerifyArgs a, int c
     __shared__ int s_arg[VD_MAX_ROWS], s_stop, s_first[4], s_last[4];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, T = a.T, rows = 2 * T + 1;
     const bool greedy = !(a.temperature > 0), sums = !greedy || a.logp;
-    const double c = vd_rate(a);
     VdWs w;
     vd_ws(a.ws, a.B, T, chunks, &w);
     vd_table(pow2);
@@ -388,10 +385,10 @@ __global__ __launch_bounds__(VD_THREADS) void vd_pick_kernel(VerifyArgs a, int c
     const double mq = sampled ? (double)s_m[rq] : 0.0, iq = sampled ? 1.0 / s_z[rq] : 0.0;
     bool residual = d.rejected;
     auto weight_of = [&](int v, float xp, float xq) -> double {
-        const double p = vd_weight(xp, mp, c, pow2) * ip;
+        const double p = vd_weight(xp, mp, a, pow2) * ip;
         if (!residual) return p;
         if (!sampled) return v == d.token ? 0.0 : p;
-        const double e = p - vd_weight(xq, mq, c, pow2) * iq;
+        const double e = p - vd_weight(xq, mq, a, pow2) * iq;
         return e > 0.0 ? e : 0.0;
     };
     // a drafted token that was not sampled leaves its own chunk without its weight: that chunk is summed again
@@ -421,7 +418,7 @@ __global__ __launch_bounds__(VD_THREADS) void vd_pick_kernel(VerifyArgs a, int c
         if (residual && sampled) return w.mass[(size_t)b * chunks + k];
         if (residual && k == own) return own_mass;
         const float cm = w.max[cell + k];
-        return cm == -INFINITY ? 0.0 : w.sum[cell + k] * vd_weight(cm, mp, c, pow2) * ip;
+        return cm == -INFINITY ? 0.0 : w.sum[cell + k] * vd_weight(cm, mp, a, pow2) * ip;
     };
     double total, v0;                             // v0: of the first 64 chunks, kept
     for (;;) {
@@ -533,8 +530,11 @@ static void vd_launch(const VerifyArgs &a, hipStream_t st) {
     }
 }
 
-void launch_verify_drafts(const VerifyArgs &a, hipStream_t st) {
+void launch_verify_drafts(const VerifyArgs &a0, hipStream_t st) {
+    VerifyArgs a = a0;
     if (a.B <= 0) return;
+    a.rate = kVdLog2e / (a.temperature > 0 ? a.temperature : 1.0);
+    a.least = kVdLeast / a.rate;
     if (vd_chunk_len(a.B, a.T, a.V) == 2048) vd_launch<32>(a, st);
     else vd_launch<8>(a, st);
 }
