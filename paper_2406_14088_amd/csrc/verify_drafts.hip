@@ -17,10 +17,30 @@
 
 #define VD_THREADS 256
 
+// Over a wavefront: within rows of 16 lanes by DPP (lane ^ 1, lane ^ 2, mirrored half row, mirrored row), then across the four rows.
+template <int CTRL>
+__device__ __forceinline__ float vd_dpp(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL>
+__device__ __forceinline__ double vd_dpp(double v) {
+    return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xf, 0xf, true), __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xf, 0xf, true));
+}
 __device__ __forceinline__ double vd_wave_sum(double v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+    v += vd_dpp<0xb1>(v);
+    v += vd_dpp<0x4e>(v);
+    v += vd_dpp<0x141>(v);
+    v += vd_dpp<0x140>(v);
+    v += __shfl_xor(v, 16, 64);
+    return v + __shfl_xor(v, 32, 64);
+}
+__device__ __forceinline__ float vd_wave_max(float v) {
+    v = fmaxf(v, vd_dpp<0xb1>(v));
+    v = fmaxf(v, vd_dpp<0x4e>(v));
+    v = fmaxf(v, vd_dpp<0x141>(v));
+    v = fmaxf(v, vd_dpp<0x140>(v));
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    return fmaxf(v, __shfl_xor(v, 32, 64));
 }
 
 static __device__ const double vd_pow2[128] = {  // 2^(k / 128)
@@ -154,7 +174,7 @@ __global__ __launch_bounds__(VD_THREADS, 8) void vd_rows_kernel(VerifyArgs a, in
     bool nan = false;
 #pragma unroll
     for (int e = 0; e < EPT; ++e) { nan |= x[e] != x[e]; m = fmaxf(m, x[e]); }
-    m = wave_max(m);
+    m = vd_wave_max(m);
     int arg = 0x7fffffff;
     if (ARG) {
 #pragma unroll
