@@ -8,11 +8,10 @@
 // relative error e move a draw to a neighbour with a probability of the order of V * e, about one in a hundred for fp32 (1e-7) and
 // V = 128256.  So weights and sums are fp64: 2^g from a table of 128 powers in LDS and a polynomial of degree 3 for the rest
 // (interpolation at the Chebyshev nodes, relative error 6e-13), 11 fp64 instructions per logit.  They take twice the time of fp32 ones and
-// bound the reading of the rows (with a polynomial of degree 8 and no table, 15 of them): 4.7 TB/s, 6.3 TB/s for the maxima alone.
+// bound the reading of the rows (with a polynomial of degree 8 and no table, 15 of them): 4.9 TB/s, 6.3 TB/s for the maxima alone.
 //
 // Measured: 64 x 5 drafts, vocabulary 32000 (90 MB): 43 us, of it 22 for the rows, 5 for the decision, 7 for the weights of the rejected row
-// and 8 for the token, the last three a chain of dependent loads each; 128 x up to 7 drafts, vocabulary 128256: 145 us (rows 108, 9, 25, 10).
-// One workgroup per sequence that decides and picks, without the kernels between, took 2.5 times as long for the second.
+// and 8 for the token, the last three a chain of dependent loads each; 128 x up to 7 drafts, vocabulary 128256: 138 us (rows 106, 9, 25, 10).
 #include "kernels.h"
 
 #define VD_THREADS 256
