@@ -135,6 +135,15 @@ def test_span_attention_weights_of_long_unsplit_sequences(T, Hq, hd, block_scale
     _check_span(cache, _rnd(g, B, T, Hq, hd, std=1.5), lens, T, 1)
 
 
+@pytest.mark.parametrize("T,Hq", [(3, 4), (4, 8), (8, 8)])
+@pytest.mark.parametrize("page", [0, 16])
+def test_span_attention_weights_of_ragged_spans(T, Hq, page):
+    B, Hkv, hd, S = 6, 2, 128, 160                     # query rows behind a sequence's last token add nothing to its weights
+    g = torch.Generator().manual_seed(T)
+    cache = R.Cache(_rnd(g, B, Hkv, S, hd), _rnd(g, B, Hkv, S, hd), False, page)
+    _check_span(cache, _rnd(g, B, T, Hq, hd), [0, 150, 31, 32, 100, 7], T, span=[1, T, 0, T - 1, 2, T + 3])
+
+
 @pytest.mark.parametrize("T,Hq", [(1, 64), (2, 64), (4, 64), (5, 64)])
 def test_span_attention_weights_of_many_sequences(T, Hq):
     B, Hkv, hd, S = 65, 8, 64, 96                      # more kv heads than workgroups of four wavefronts run at once
