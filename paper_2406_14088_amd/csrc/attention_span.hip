@@ -14,8 +14,11 @@
 // contraction index 8 j + i, of the second 8 j + 4 + i.
 //
 // One pass with a running maximum and sum per query row.  The maximum is raised (and the accumulators rescaled) only when a score
-// exceeds it by more than 2^8, so that most tiles need no reduction across lanes: weights up to 2^8 are as exact in two half terms as
-// weights up to 1.  Scores are kept in units of log 2 (q is scaled by log2(e) / sqrt(hd) before it is split).
+// exceeds it by more than 2^8, so that most tiles need no reduction across lanes.  A weight at the maximum enters the products as 2^7 (half rows:
+// the maximum is taken 7 lower; block-scaled: with the reference of the row scales), the largest as 2^15: weights from 2^-10 of the maximum on keep
+// about 22 bits, smaller ones are rounded to nearest on a grid of 2^-31, so that thousands of rows with little weight each do not lose any
+// on average (at their own size, cut off, rows 2^-17 below the maximum lost 0.4 % of theirs).  Scores are kept in units of log 2 (q is scaled by
+// log2(e) / sqrt(hd) before it is split).
 //
 // Memory: bound by reading K and V once.  Each wavefront copies V tiles from HBM into its own two-stage LDS ring (buffer loads with the
 // LDS destination, 16 rows per buffer descriptor: pages hold a multiple of 16 rows; rows past the end arrive as zeros), so no barrier is
@@ -39,11 +42,13 @@
 #include <type_traits>
 
 #define SPAN_LDS(p) ((__attribute__((address_space(3))) void *)(p))
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
 static constexpr int kSpanTile = 32;        // cache rows per tile
 static constexpr float kSpanSlack = 8.f;    // how far (in powers of two) a weight may exceed the running reference
+static constexpr float kSpanShift = 7.f, kSpanUnit = 128.f;  // the reference as the matrix cores see it: 2^7, its log2
 
 __device__ __forceinline__ float span_ror8(float v) {  // lane l of a row of 16 receives lane (l + 8) % 16
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xf, 0xf, true));
@@ -113,6 +118,7 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
     constexpr int TILEB = kSpanTile * RB;
     constexpr bool KL = RT == 2;                  // K through LDS as well
     constexpr bool EARLY = KL || !WT;
+    constexpr float SHIFT = I16 ? 0.f : kSpanShift;  // half rows: weights are exp2(score - (maximum - SHIFT)) from the start, sums included
     constexpr int NV = RT ? 8 : 4, KEEP = WT == 2 ? (RT ? 8 : 16) : 0;  // scores of a lane per tile and column tile
     constexpr int SCALES = KL ? 2 * TILEB : TILEB, STAGE = SCALES + (I16 ? 512 : 0);  // a V tile, with KL a K tile, the row scales of K and V
     constexpr int LPR = RB / 16;                  // lanes per row of a copy instruction
@@ -434,13 +440,12 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[nt][t][i] *= alpha;
             }
-            const float m = mrun[nt] == -INFINITY ? 0.f : mrun[nt];  // nothing seen yet: all weights are 0
+            const float m = mrun[nt] == -INFINITY ? 0.f : mrun[nt] - SHIFT;  // nothing seen yet: all weights are 0
             float wmax = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v[e] = __builtin_amdgcn_exp2f(v[e] - m);
-                den[nt] += v[e];
-            }
+            for (int e = 0; e < 8; ++e) v[e] = __builtin_amdgcn_exp2f(v[e] - m);
+            // the tile's sum first: added one by one to a large sum, equal small weights are all rounded the same way
+            den[nt] += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
             float inv = 1.f;
             if (I16) {
                 // The row scale of V rides on the probability.  Scales are far below the normal range of a half, so the weights are
@@ -460,13 +465,13 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
 #pragma unroll
                         for (int i = 0; i < 4; ++i) acc[nt][t][i] *= beta;
                 }
-                inv = ref[nt] > 0.f ? __builtin_amdgcn_rcpf(ref[nt]) : 0.f;
+                inv = ref[nt] > 0.f ? kSpanUnit * __builtin_amdgcn_rcpf(ref[nt]) : 0.f;
             }
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {      // the high term cut off, the low term takes what is left
+            for (int e = 0; e < 8; e += 2) {      // the high term cut off, the low term takes what is left, rounded to nearest
                 const float x0 = I16 ? v[e] * inv : v[e], x1 = I16 ? v[e + 1] * inv : v[e + 1];
                 const f16x2_t hi = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_pkrtz(x0, x1));
-                const f16x2_t lo = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_pkrtz(x0 - (float)hi.x, x1 - (float)hi.y));
+                const f16x2_t lo = __builtin_convertvector(f32x2_t{x0 - (float)hi.x, x1 - (float)hi.y}, f16x2_t);
                 pf[nt][e] = RT || c < 8 ? hi.x : lo.x;
                 pf[nt][e + 1] = RT || c < 8 ? hi.y : lo.y;
                 if (RT) { pl[RT ? nt : 0][e] = lo.x; pl[RT ? nt : 0][e + 1] = lo.y; }
@@ -528,13 +533,13 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
         float d = den[nt];
         d += __shfl_xor(d, 16, 64);
         d += __shfl_xor(d, 32, 64);
-        if (j == 0 && c < TR) { s_max(wave, TR * nt + c) = mrun[nt]; s_den(wave, TR * nt + c) = d; }
+        if (j == 0 && c < TR) { s_max(wave, TR * nt + c) = mrun[nt] - SHIFT; s_den(wave, TR * nt + c) = d; }
 #pragma unroll
         for (int t = 0; t < OT; ++t) {
             f32x4_t o;
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] = RT ? acc[nt][t][i] : acc[nt][t][i] + span_ror8(acc[nt][t][i]);
-            if (I16) o = o * (ref[nt] * 64.f);
+            if (I16) o = o * (ref[nt] * (64.f / kSpanUnit));
             if (c < TR) *reinterpret_cast<f32x4_t *>(part + (TR * nt + c) * HD + 16 * t + 4 * j) = o;
         }
     }

@@ -1,0 +1,50 @@
+"""Span attention against its definition in 64 bits, element by element: each output and each weight within what the formats and sums of
+its own row allow (tests/ref_span_bounds.py; tests/test_span_bounds_host.py shows on the CPU that a second half term left out or probabilities split
+at their own size are several times beyond that)."""
+import math
+
+import pytest
+import torch
+
+from tests.gpu_util import DEV
+from tests import ref_span as R
+from tests import ref_span_bounds as E
+from tests.test_gpu_span_ops import _i32, _ops, _rnd, _run_span
+
+pytestmark = pytest.mark.gpu
+
+
+def _check(cache, q, lens, T, nsplit=0, span=None, weights=True):
+    q = q.float().double()
+    k, v = cache.values(0), cache.values(1)
+    want, hi, both, add, add_tol = E.attend(q, k, v, lens, T, cache.block_scaled, span)
+    w0 = torch.rand((cache.B, cache.Hkv, cache.S), generator=torch.Generator().manual_seed(6)) * 0.1
+    weight = w0.to(DEV) if weights else None
+    out, lo = _run_span(cache, q, lens, T, nsplit, span, weight)
+    there = ~want.isnan()
+    assert ((out - want).abs() <= hi)[there].all(), float(((out - want).abs() / hi)[there].max())
+    assert ((out + lo - want).abs() <= both)[there].all(), float(((out + lo - want).abs() / both)[there].max())
+    assert (out[~there] == 7.0).all() and (lo[~there] == 7.0).all()
+    if weights:      # the query rows of a kv head are added up in fp32, at most T * Hq / Hkv of them, and to what was there
+        ref = w0.double() + add
+        tol = add_tol + (math.sqrt(T * q.shape[2] / cache.Hkv) * 4 * add + 2 * ref) * R.F32_STEP
+        assert ((weight.cpu().double() - ref).abs() <= tol).all()
+        assert torch.equal(weight.cpu()[add == 0], w0[add == 0])
+
+
+SHAPES = [(1, 4, 1), (3, 4, 1), (6, 4, 1), (6, 8, 1), (2, 8, 2)]       # T, Hq, Hkv: 4, 12, 24, 48 query rows of a kv head (two workgroups), 8
+
+
+@pytest.mark.parametrize("nsplit", [1, 3])
+@pytest.mark.parametrize("block_scaled", [False, True])
+@pytest.mark.parametrize("T,Hq,Hkv", SHAPES)
+def test_rows_with_little_weight_each(T, Hq, Hkv, block_scaled, nsplit):
+    """The first row takes most of the weight and is zero but for one element, thousands of others share the rest: a bounded cache's usual shape."""
+    hd, n = 128, 8200
+    S = n + 8
+    g = torch.Generator().manual_seed(T + Hq)
+    q0 = (_rnd(g, 1, 1, 1, hd) * 1.5).expand(1, T, Hq, hd) * (0.9 + 0.05 * torch.arange(T * Hq, dtype=torch.float64).view(1, T, Hq, 1) % 0.4)
+    k, v = _rnd(g, 1, Hkv, S, hd) * 0.02, 1 + 0.1 * _rnd(g, 1, Hkv, S, hd)
+    k[:, :, 0] = q0[0, 0, 0] / (q0[0, 0, 0] ** 2).sum() * hd ** 0.5 * 12.0
+    v[:, :, 0], v[:, :, 0, 0] = 0, 1
+    _check(R.Cache(k, v, block_scaled), q0, [n - T], T, nsplit)
