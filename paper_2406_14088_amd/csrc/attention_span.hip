@@ -435,8 +435,9 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
                 const float alpha = mrun[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mrun[nt] - mnew);
                 mrun[nt] = mnew;
                 den[nt] *= alpha;
+                if (I16) ref[nt] *= alpha;        // the accumulators count in it
 #pragma unroll
-                for (int t = 0; t < OT; ++t)
+                for (int t = 0; t < OT && !I16; ++t)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[nt][t][i] *= alpha;
             }
@@ -449,7 +450,8 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
             float inv = 1.f;
             if (I16) {
                 // The row scale of V rides on the probability.  Scales are far below the normal range of a half, so the weights are
-                // measured in a reference per query row that follows their largest.
+                // measured in a reference per query row that follows their largest, and falls as the maximum rises: rows that have lost
+                // their weight must not set the grid for those that took it.
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int key = key0 + 16 * (e >> 2) + 4 * j + (e & 3);

@@ -1,6 +1,6 @@
 """Span attention against its definition in 64 bits, element by element: each output and each weight within what the formats and sums of
-its own row allow (tests/ref_span_bounds.py; tests/test_span_bounds_host.py shows on the CPU that a second half term left out or probabilities split
-at their own size are several times beyond that)."""
+its own row allow (tests/ref_span_bounds.py; tests/test_span_bounds_host.py shows on the CPU that a second half term left out, probabilities split
+at their own size or a stale reference of block-scaled rows are several times beyond that)."""
 import math
 
 import pytest
@@ -48,3 +48,18 @@ def test_rows_with_little_weight_each(T, Hq, Hkv, block_scaled, nsplit):
     k[:, :, 0] = q0[0, 0, 0] / (q0[0, 0, 0] ** 2).sum() * hd ** 0.5 * 12.0
     v[:, :, 0], v[:, :, 0, 0] = 0, 1
     _check(R.Cache(k, v, block_scaled), q0, [n - T], T, nsplit)
+
+
+@pytest.mark.parametrize("at", [40, 300])
+@pytest.mark.parametrize("block_scaled", [False, True])
+@pytest.mark.parametrize("T,Hq,Hkv", SHAPES)
+def test_a_late_row_of_small_values_takes_all_the_weight(T, Hq, Hkv, block_scaled, at):
+    """A row behind the first tile of a wavefront's share dominates and holds values far below those of the rows before it."""
+    hd, n = 128, 520
+    g = torch.Generator().manual_seed(T * Hq + at)
+    q = (_rnd(g, 1, 1, 1, hd) * 1.5).expand(1, T, Hq, hd)
+    for small in (10.0, 0.1, 0.01):
+        k, v = _rnd(g, 1, Hkv, n + T, hd), _rnd(g, 1, Hkv, n + T, hd) * (1e6 if block_scaled else 1e4)
+        k[:, :, at] = q[0, 0, 0] / (q[0, 0, 0] ** 2).sum() * hd ** 0.5 * 60.0
+        v[:, :, at] = small * _rnd(g, 1, Hkv, hd)
+        _check(R.Cache(k, v, block_scaled), q, [n], T, 1)

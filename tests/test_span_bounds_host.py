@@ -1,5 +1,5 @@
-"""The element-wise bound for span attention: the emulated number formats keep it, and every second half term, and the scale
-of the probabilities, is needed for that.  No GPU."""
+"""The element-wise bound for span attention: the emulated number formats keep it, and every second half term, the scale of the
+probabilities and the reference of block-scaled rows is needed for that.  No GPU."""
 import pytest
 import torch
 
@@ -14,7 +14,7 @@ def _quantised(x):
 def _data(kind, seed, scaled):
     g = torch.Generator().manual_seed(seed)
     hd = 128
-    n, R = dict(plain=(200, 8), sink=(8200, 4))[kind]
+    n, R = dict(plain=(200, 8), sink=(8200, 4), late=(220, 4))[kind]
     q = (torch.randn((R, hd), generator=g, dtype=torch.float64) * 1.5).float().double()
     k, v = (torch.randn((n, hd), generator=g, dtype=torch.float64) for _ in range(2))
     if kind == "sink":      # the first row takes most of the weight and is zero but for one element, the others have little weight and a mean of one
@@ -24,6 +24,11 @@ def _data(kind, seed, scaled):
         k[0] = q[0] / (q[0] ** 2).sum() * hd ** 0.5 * 12.0
         v = 1 + 0.1 * v
         v[0], v[0, 0] = 0, 1
+    if kind == "late":      # a row in the middle of a wavefront's share takes all the weight; its values are far below the others'
+        q[1:] = q[0]
+        k[40] = q[0] / (q[0] ** 2).sum() * hd ** 0.5 * 60.0
+        v *= 1e6
+        v[40] = 10.0 ** -(seed % 3 - 1) * torch.randn(hd, generator=g, dtype=torch.float64)
     if not scaled:
         return q, k.half().double(), v.clamp(-60000, 60000).half().double(), None
     rows = [_quantised(k), _quantised(v)]
@@ -41,7 +46,7 @@ def _worst(kind, seed, scaled, mistake=None):
     return worst
 
 
-@pytest.mark.parametrize("kind, scaled", [("plain", False), ("plain", True), ("sink", False), ("sink", True)])
+@pytest.mark.parametrize("kind, scaled", [("plain", False), ("plain", True), ("sink", False), ("sink", True), ("late", True)])
 def test_the_formats_keep_the_bound(kind, scaled):
     for seed in range(3):
         assert _worst(kind, seed, scaled) <= 1
@@ -49,7 +54,7 @@ def test_the_formats_keep_the_bound(kind, scaled):
 
 @pytest.mark.parametrize("kind, scaled, mistake", [
     ("plain", False, "q"), ("plain", True, "q"), ("plain", False, "p"), ("plain", True, "p"), ("plain", True, "rows"),
-    ("sink", False, "tail"), ("sink", True, "tail"), ("sink", False, "p")])
+    ("sink", False, "tail"), ("sink", True, "tail"), ("sink", False, "p"), ("late", True, "reference"), ("late", True, "rows")])
 def test_the_bound_sees_what_is_missing(kind, scaled, mistake):
     for seed in range(3):
         assert _worst(kind, seed, scaled, mistake) > 1
