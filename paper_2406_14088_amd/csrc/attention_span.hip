@@ -48,6 +48,7 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
 static constexpr int kSpanTile = 32;        // cache rows per tile
 static constexpr float kSpanSlack = 8.f;    // how far (in powers of two) a weight may exceed the running reference
+static constexpr float kSpanLeast = 0x1p-100f;  // values of weights times row scales below it count as zero: far below any half, and a subnormal has no reciprocal
 static constexpr float kSpanShift = 7.f, kSpanUnit = 128.f;  // the reference as the matrix cores see it: 2^7, its log2
 
 __device__ __forceinline__ float span_ror8(float v) {  // lane l of a row of 16 receives lane (l + 8) % 16
@@ -467,7 +468,7 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
 #pragma unroll
                         for (int i = 0; i < 4; ++i) acc[nt][t][i] *= beta;
                 }
-                inv = ref[nt] > 0.f ? kSpanUnit * __builtin_amdgcn_rcpf(ref[nt]) : 0.f;
+                inv = ref[nt] > kSpanLeast ? kSpanUnit * __builtin_amdgcn_rcpf(ref[nt]) : 0.f;
             }
 #pragma unroll
             for (int e = 0; e < 8; e += 2) {      // the high term cut off, the low term takes what is left, rounded to nearest

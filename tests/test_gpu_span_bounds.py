@@ -63,3 +63,13 @@ def test_a_late_row_of_small_values_takes_all_the_weight(T, Hq, Hkv, block_scale
         k[:, :, at] = q[0, 0, 0] / (q[0, 0, 0] ** 2).sum() * hd ** 0.5 * 60.0
         v[:, :, at] = small * _rnd(g, 1, Hkv, hd)
         _check(R.Cache(k, v, block_scaled), q, [n], T, 1)
+
+
+@pytest.mark.parametrize("T,Hq,Hkv", SHAPES)
+def test_values_below_the_normal_numbers(T, Hq, Hkv):
+    """Block-scaled rows whose scale is a subnormal number, alone and beside rows of ordinary size."""
+    hd, n = 64, 150
+    g = torch.Generator().manual_seed(T * Hq)
+    k, v, q = _rnd(g, 2, Hkv, n + T, hd), _rnd(g, 2, Hkv, n + T, hd) * 1e-36, _rnd(g, 2, T, Hq, hd)
+    v[1, :, ::5] *= 1e36
+    _check(R.Cache(k, v, True), q, [n, n - 70], T)
