@@ -267,8 +267,10 @@ int rl_op_rope_append_at(const float *qkv, int32_t nsplit, size_t split_stride, 
  * nsplit: workgroups that share the rows of a sequence, 1 .. 64, or 0: chosen from the shape.  ws: fp32 workspace of ws_floats
  * elements, 16-byte aligned, at least rl_op_span_attention_ws_floats(same arguments, weights = whether weight is given) of them (else
  * RL_GEN_E_CAPACITY; may be NULL when that is 0).
- * A query sees a row whose K or V is not finite as a non-finite score or value; rows that a query does not see never reach
- * its result, whatever they hold.  Hq/Hkv <= 64. */
+ * A query that holds a NaN, or sees a row whose K or V does, gives NaN in out and out_lo (from q or K: also in weight); a block-scaled row counts as one
+ * whose scale is not finite.  An infinite half in V gives NaN or the largest half of its sign, one in K a score that is infinite or NaN.  Rows that a
+ * query does not see never reach its result, whatever they hold.  q times log2(e) / sqrt(hd) saturates at +-131008, out and out_lo at
+ * +-65504.  Hq/Hkv <= 64. */
 int rl_op_span_attention(const float *q, const uint16_t *kc, const uint16_t *vc, const float *kscale, const float *vscale,
                          const int32_t *table, int32_t table_stride, int32_t page_size, const int32_t *d_len, const int32_t *d_span,
                          uint16_t *out, uint16_t *out_lo, float *weight, float *ws, size_t ws_floats, int32_t B, int32_t T, int32_t Hq,

@@ -49,7 +49,7 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 static constexpr int kSpanTile = 32;        // cache rows per tile
 static constexpr float kSpanSlack = 8.f;    // how far (in powers of two) a weight may exceed the running reference
 static constexpr float kSpanLeast = 0x1p-100f;  // values of weights times row scales below it count as zero: far below any half, and a subnormal has no reciprocal
-static constexpr float kSpanShift = 7.f, kSpanUnit = 128.f;  // the reference as the matrix cores see it: 2^7, its log2
+static constexpr float kSpanShift = 7.f, kSpanUnit = 128.f;  // the reference in the products: 2^7, as exponent and factor
 
 __device__ __forceinline__ float span_ror8(float v) {  // lane l of a row of 16 receives lane (l + 8) % 16
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xf, 0xf, true));
@@ -63,6 +63,11 @@ __device__ __forceinline__ float span_max_groups(float v) {  // over the four la
     v = fmaxf(v, __shfl_xor(v, 16, 64));
     return fmaxf(v, __shfl_xor(v, 32, 64));
 }
+
+// Saturating, like every half here, and a NaN stays one (v_med3 takes it for the lower limit).
+__device__ __forceinline__ _Float16 span_half(float v) { return (_Float16)(v != v ? v : __builtin_amdgcn_fmed3f(v, -65504.f, 65504.f)); }
+__device__ __forceinline__ uint32_t span_pack(float x0, float x1) { return __builtin_bit_cast(uint32_t, f16x2_t{span_half(x0), span_half(x1)}); }
+__device__ __forceinline__ uint32_t span_pack_lo(float x0, float x1, uint32_t hi) { return span_pack(x0 - f16lo_to_f32(hi), x1 - f16hi_to_f32(hi)); }
 
 // Eight int16 elements n = 64 h + l as h and l / 64.
 __device__ __forceinline__ void span_split(u32x4_t n, f16x8_t *h, f16x8_t *l) {
@@ -277,6 +282,7 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
     // ---- Q^T operands: column c of tile nt = query row r0 + TR nt + c % TR; k-step s covers elements 32 s + 8 j + 0..7
     f16x8_t qf[NT][KS], ql[RT ? NT : 1][RT ? KS : 1];
     const float qscale = rsqrtf((float)HD) * 1.44269504f;
+    float finite = 0.f;                           // NaN once an element is not
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -288,7 +294,17 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
                 const _Float16 lo = (_Float16)__builtin_amdgcn_fmed3f(v - (float)hi, -65504.f, 65504.f);
                 qf[nt][s][e] = RT || c < 8 ? hi : lo;
                 if (RT) ql[RT ? nt : 0][RT ? s : 0][e] = lo;
+                finite = __builtin_fmaf(v, 0.f, finite);
             }
+    if (__any(finite != 0.f)) {                   // rare, and kept out of the way of the first tile: the limits above take a NaN for the lower one
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (row_ok[nt] && qraw[nt][2 * s + (e >> 2)][e & 3] != qraw[nt][2 * s + (e >> 2)][e & 3]) qf[nt][s][e] = (_Float16)__builtin_nanf("");
+    }
 
     int vaddr[OT], kaddr[KL ? KS : 1];
 #pragma unroll
@@ -349,6 +365,8 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 ksc[h] = *reinterpret_cast<const f32x4_t *>(st + SCALES + 64 * h + 16 * j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ksc[h][i] = __builtin_fmaf(ksc[h][i], 64.f, ksc[h][i] * 0.f);  // infinite: NaN, as inf - inf over the row's elements is
                 vsc[h] = *reinterpret_cast<const f32x4_t *>(st + SCALES + 256 + 64 * h + 16 * j);
             }
         }
@@ -405,7 +423,7 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
             for (int e = 0; e < 8; ++e) {
                 float x = sacc[nt][e >> 2][e & 3];
                 if (!RT) x += span_ror8(x);       // high and low term of the query row
-                if (I16) x *= ksc[e >> 2][e & 3] * 64.f;
+                if (I16) x *= ksc[e >> 2][e & 3];
                 v[e] = x;
             }
             if (tail) {
@@ -584,8 +602,8 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
             u32x4_t h, l;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                h[e] = pack_f16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
-                l[e] = pack_f16x2_lo(o[2 * e] * inv, o[2 * e + 1] * inv, h[e]);
+                h[e] = span_pack(o[2 * e] * inv, o[2 * e + 1] * inv);
+                l[e] = span_pack_lo(o[2 * e] * inv, o[2 * e + 1] * inv, h[e]);
             }
             *reinterpret_cast<u32x4_t *>(a.out + at) = h;
             if (a.out_lo) *reinterpret_cast<u32x4_t *>(a.out_lo + at) = l;
@@ -701,13 +719,13 @@ __global__ __launch_bounds__(256) void span_join_kernel(SpanArgs a, int merge_bl
         const float inv = 1.0f / d;
         const size_t at = (((size_t)b * a.T + rr / G) * a.Hq + kvh * G + rr % G) * HD + lane * PER;
         if (PER == 2) {
-            const uint32_t h = pack_f16x2(o0 * inv, o1 * inv);
+            const uint32_t h = span_pack(o0 * inv, o1 * inv);
             *reinterpret_cast<uint32_t *>(a.out + at) = h;
-            if (a.out_lo) *reinterpret_cast<uint32_t *>(a.out_lo + at) = pack_f16x2_lo(o0 * inv, o1 * inv, h);
+            if (a.out_lo) *reinterpret_cast<uint32_t *>(a.out_lo + at) = span_pack_lo(o0 * inv, o1 * inv, h);
         } else {
-            const f16_t h = f32_to_f16(o0 * inv);
-            a.out[at] = h;
-            if (a.out_lo) a.out_lo[at] = f32_to_f16(o0 * inv - f16_to_f32(h));
+            const _Float16 h = span_half(o0 * inv);
+            a.out[at] = __builtin_bit_cast(f16_t, h);
+            if (a.out_lo) a.out_lo[at] = __builtin_bit_cast(f16_t, span_half(o0 * inv - (float)h));
         }
         return;
     }

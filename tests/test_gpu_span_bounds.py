@@ -73,3 +73,52 @@ def test_values_below_the_normal_numbers(T, Hq, Hkv):
     k, v, q = _rnd(g, 2, Hkv, n + T, hd), _rnd(g, 2, Hkv, n + T, hd) * 1e-36, _rnd(g, 2, T, Hq, hd)
     v[1, :, ::5] *= 1e36
     _check(R.Cache(k, v, True), q, [n, n - 70], T)
+
+
+@pytest.mark.parametrize("block_scaled", [False, True])
+@pytest.mark.parametrize("T,Hq,Hkv,nsplit", [(1, 4, 1, 1), (3, 4, 1, 1), (6, 4, 1, 1), (12, 4, 1, 1), (2, 4, 1, 2), (6, 4, 1, 2)])
+def test_not_a_number_comes_out_as_one(T, Hq, Hkv, nsplit, block_scaled):
+    """A NaN in a query, a K or a V row makes the queries that hold or see it NaN, and no others differ in a bit."""
+    hd, n = 128, 270
+    g = torch.Generator().manual_seed(T)
+    k, v, q = _rnd(g, 2, Hkv, n + T, hd), _rnd(g, 2, Hkv, n + T, hd), _rnd(g, 2, T, Hq, hd)
+    clean, clean_lo = _run_span(R.Cache(k, v, block_scaled), q, [n, n - 9], T, nsplit)
+    bad = q.clone()
+    bad[0, T - 1, 2, 5] = float("nan")
+    hit = torch.zeros((2, T, Hq), dtype=torch.bool)
+    hit[0, T - 1, 2] = True
+    for name, at in (("q", 0), ("k", 40), ("v", 40), ("k", n + T - 1), ("v", n + T - 1)):
+        cache = R.Cache(k, v, block_scaled)
+        if name != "q":
+            i = "kv".index(name)
+            if block_scaled:
+                cache.scales[i][0, 0, at] = float("nan")
+            else:
+                cache.rows[i][0, 0, at] = float("nan")
+            hit = torch.zeros((2, T, Hq), dtype=torch.bool)
+            hit[0, max(0, at - n):] = True
+        out, lo = _run_span(cache, bad if name == "q" else q, [n, n - 9], T, nsplit)
+        assert out[hit].isnan().all() and lo[hit].isnan().all(), (name, at)
+        assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lo[~hit], clean_lo[~hit]), (name, at)
+
+
+@pytest.mark.parametrize("block_scaled", [False, True])
+def test_an_infinite_value_is_no_finite_result(block_scaled):
+    T, Hq, hd, n = 3, 4, 64, 100
+    g = torch.Generator().manual_seed(2)
+    k, v, q = _rnd(g, 1, 1, n + T, hd), _rnd(g, 1, 1, n + T, hd), _rnd(g, 1, T, Hq, hd)
+    for sign in (1, -1):
+        for at in (5, n, n + 2):
+            cache = R.Cache(k, v, block_scaled)
+            if block_scaled:
+                cache.scales[1][0, 0, at] = sign * float("inf")
+            else:
+                cache.rows[1][0, 0, at] = sign * float("inf")
+            out, _ = _run_span(cache, q, [n], T)
+            sees = out[0, max(0, at - n):]
+            # NaN, or saturated with the sign of the value; a row whose scale is infinite has values of both signs
+            assert (sees.isnan() | (sees == sign * 65504)).all() and (not block_scaled or sees.isnan().all())
+            if block_scaled:
+                cache = R.Cache(k, v, True)
+                cache.scales[0][0, 0, at] = sign * float("inf")
+                assert _run_span(cache, q, [n], T)[0][0, max(0, at - n):].isnan().all()
