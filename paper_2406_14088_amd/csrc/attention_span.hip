@@ -64,11 +64,6 @@ __device__ __forceinline__ float span_max_groups(float v) {  // over the four la
     return fmaxf(v, __shfl_xor(v, 32, 64));
 }
 
-// Saturating, like every half here, and a NaN stays one (v_med3 takes it for the lower limit).
-__device__ __forceinline__ _Float16 span_half(float v) { return (_Float16)(v != v ? v : __builtin_amdgcn_fmed3f(v, -65504.f, 65504.f)); }
-__device__ __forceinline__ uint32_t span_pack(float x0, float x1) { return __builtin_bit_cast(uint32_t, f16x2_t{span_half(x0), span_half(x1)}); }
-__device__ __forceinline__ uint32_t span_pack_lo(float x0, float x1, uint32_t hi) { return span_pack(x0 - f16lo_to_f32(hi), x1 - f16hi_to_f32(hi)); }
-
 // Eight int16 elements n = 64 h + l as h and l / 64.
 __device__ __forceinline__ void span_split(u32x4_t n, f16x8_t *h, f16x8_t *l) {
     typedef uint16_t u16x8_t __attribute__((ext_vector_type(8)));
@@ -602,8 +597,8 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
             u32x4_t h, l;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                h[e] = span_pack(o[2 * e] * inv, o[2 * e + 1] * inv);
-                l[e] = span_pack_lo(o[2 * e] * inv, o[2 * e + 1] * inv, h[e]);
+                h[e] = pack_f16x2_nan(o[2 * e] * inv, o[2 * e + 1] * inv);
+                l[e] = pack_f16x2_lo_nan(o[2 * e] * inv, o[2 * e + 1] * inv, h[e]);
             }
             *reinterpret_cast<u32x4_t *>(a.out + at) = h;
             if (a.out_lo) *reinterpret_cast<u32x4_t *>(a.out_lo + at) = l;
@@ -719,13 +714,13 @@ __global__ __launch_bounds__(256) void span_join_kernel(SpanArgs a, int merge_bl
         const float inv = 1.0f / d;
         const size_t at = (((size_t)b * a.T + rr / G) * a.Hq + kvh * G + rr % G) * HD + lane * PER;
         if (PER == 2) {
-            const uint32_t h = span_pack(o0 * inv, o1 * inv);
+            const uint32_t h = pack_f16x2_nan(o0 * inv, o1 * inv);
             *reinterpret_cast<uint32_t *>(a.out + at) = h;
-            if (a.out_lo) *reinterpret_cast<uint32_t *>(a.out_lo + at) = span_pack_lo(o0 * inv, o1 * inv, h);
+            if (a.out_lo) *reinterpret_cast<uint32_t *>(a.out_lo + at) = pack_f16x2_lo_nan(o0 * inv, o1 * inv, h);
         } else {
-            const _Float16 h = span_half(o0 * inv);
+            const _Float16 h = f32_to_half_nan(o0 * inv);
             a.out[at] = __builtin_bit_cast(f16_t, h);
-            if (a.out_lo) a.out_lo[at] = __builtin_bit_cast(f16_t, span_half(o0 * inv - (float)h));
+            if (a.out_lo) a.out_lo[at] = __builtin_bit_cast(f16_t, f32_to_half_nan(o0 * inv - (float)h));
         }
         return;
     }

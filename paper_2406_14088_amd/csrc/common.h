@@ -104,6 +104,13 @@ __device__ __forceinline__ uint32_t pack_f16x2_lo(float x0, float x1, uint32_t h
     return pack_f16x2(x0 - f16lo_to_f32(hi), x1 - f16hi_to_f32(hi));
 }
 
+// The same conversions, saturating, but a NaN stays one (v_med3 takes it for the lower limit).
+__device__ __forceinline__ _Float16 f32_to_half_nan(float v) { return (_Float16)(v != v ? v : __builtin_amdgcn_fmed3f(v, -65504.f, 65504.f)); }
+__device__ __forceinline__ uint32_t pack_f16x2_nan(float x0, float x1) { return __builtin_bit_cast(uint32_t, f16x2_t{f32_to_half_nan(x0), f32_to_half_nan(x1)}); }
+__device__ __forceinline__ uint32_t pack_f16x2_lo_nan(float x0, float x1, uint32_t hi) {
+    return pack_f16x2_nan(x0 - f16lo_to_f32(hi), x1 - f16hi_to_f32(hi));
+}
+
 // g / (1 + e^-g) * u.  e^-g = 2^t with the rounding error of t = -g log2(e) carried to first order; the quotient by the hardware's
 // reciprocal and one correction with its remainder: the accuracy of expf and an IEEE division at half their instructions.  Below
 // g = -87 the factor of g stays at e^-87 (1.6e-38: nothing in a half for any gate and up sum that halves can produce), above 100 at 1.

@@ -58,12 +58,20 @@ __global__ __launch_bounds__(256) void rope_append_at_kernel(RopeAppendAtArgs a)
         }
     }
     float am = 0.f;
-    if (SCALED) {
+    if (SCALED) {  // the largest magnitude by its bits: a NaN is above everything and gives a row whose scale is one
+        uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) am = fmaxf(am, fmaxf(fabsf(x[i]), fabsf(y[i])));
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t p = __float_as_uint(x[i]) & 0x7fffffffu, q = __float_as_uint(y[i]) & 0x7fffffffu, r = p > q ? p : q;
+            top = r > top ? r : top;
+        }
 #pragma unroll
-        for (int o = 1; o < 8; o <<= 1) am = fmaxf(am, __shfl_xor(am, o, 64));
-        if (hd == 128) am = fmaxf(am, __shfl_xor(am, 8, 64));
+        for (int o = 1; o < 16; o <<= 1) {
+            if (o == 8 && hd != 128) break;
+            const uint32_t r = __shfl_xor(top, o, 64);
+            top = r > top ? r : top;
+        }
+        am = __uint_as_float(top);
     }
     if (!valid) return;
     if (kind == 0) {
@@ -73,12 +81,12 @@ __global__ __launch_bounds__(256) void rope_append_at_kernel(RopeAppendAtArgs a)
             *reinterpret_cast<f32x4_t *>(a.q_f32 + o + e1) = y;
         }
         if (a.q_f16) {
-            const u32x2_t hx = {pack_f16x2(x.x, x.y), pack_f16x2(x.z, x.w)}, hy = {pack_f16x2(y.x, y.y), pack_f16x2(y.z, y.w)};
+            const u32x2_t hx = {pack_f16x2_nan(x.x, x.y), pack_f16x2_nan(x.z, x.w)}, hy = {pack_f16x2_nan(y.x, y.y), pack_f16x2_nan(y.z, y.w)};
             *reinterpret_cast<u32x2_t *>(a.q_f16 + o + e0) = hx;
             *reinterpret_cast<u32x2_t *>(a.q_f16 + o + e1) = hy;
             if (a.q_f16_lo) {
-                *reinterpret_cast<u32x2_t *>(a.q_f16_lo + o + e0) = u32x2_t{pack_f16x2_lo(x.x, x.y, hx.x), pack_f16x2_lo(x.z, x.w, hx.y)};
-                *reinterpret_cast<u32x2_t *>(a.q_f16_lo + o + e1) = u32x2_t{pack_f16x2_lo(y.x, y.y, hy.x), pack_f16x2_lo(y.z, y.w, hy.y)};
+                *reinterpret_cast<u32x2_t *>(a.q_f16_lo + o + e0) = u32x2_t{pack_f16x2_lo_nan(x.x, x.y, hx.x), pack_f16x2_lo_nan(x.z, x.w, hx.y)};
+                *reinterpret_cast<u32x2_t *>(a.q_f16_lo + o + e1) = u32x2_t{pack_f16x2_lo_nan(y.x, y.y, hy.x), pack_f16x2_lo_nan(y.z, y.w, hy.y)};
             }
         }
         return;
@@ -93,8 +101,8 @@ __global__ __launch_bounds__(256) void rope_append_at_kernel(RopeAppendAtArgs a)
         hy = u32x2_t{pack_i16x2(kv_quant(y.x, inv), kv_quant(y.y, inv)), pack_i16x2(kv_quant(y.z, inv), kv_quant(y.w, inv))};
         if (u == 0) (kind == 1 ? a.map.kscale : a.map.vscale)[rowi] = kv_scale_of(am);
     } else {
-        hx = u32x2_t{pack_f16x2(x.x, x.y), pack_f16x2(x.z, x.w)};
-        hy = u32x2_t{pack_f16x2(y.x, y.y), pack_f16x2(y.z, y.w)};
+        hx = u32x2_t{pack_f16x2_nan(x.x, x.y), pack_f16x2_nan(x.z, x.w)};
+        hy = u32x2_t{pack_f16x2_nan(y.x, y.y), pack_f16x2_nan(y.z, y.w)};
     }
     *reinterpret_cast<u32x2_t *>(dst + e0) = hx;
     *reinterpret_cast<u32x2_t *>(dst + e1) = hy;

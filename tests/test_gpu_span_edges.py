@@ -1,0 +1,44 @@
+"""Edges of the operators for steps of several tokens that their own tests leave out: numbers that are none, the long paths of draft
+verification, workspaces of larger batches, operands that do not fit."""
+import pytest
+import torch
+
+from tests.gpu_util import DEV
+from tests import ref_span as R
+from tests.test_gpu_span_ops import _i32, _ops, _rnd, _table
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("hd,rot,style", [(64, 64, 1), (128, 64, 0), (128, 128, 1)])
+@pytest.mark.parametrize("block_scaled", [False, True])
+def test_append_keeps_not_a_number(block_scaled, hd, rot, style):
+    """A NaN in a query, key or value reaches the elements it turns with (block-scaled: its row) and nothing else differs in a bit."""
+    B, T, Hq, Hkv, S = 2, 3, 4, 2, 32
+    g = torch.Generator().manual_seed(hd + rot)
+    heads = Hq + 2 * Hkv
+    clean = _rnd(g, B * T, heads, hd).float()
+    bad = clean.clone()
+    hit = torch.zeros((B * T, heads, hd), dtype=torch.bool)
+    for m, head, e in ((1, 2, 5), (2, Hq + 1, 7), (4, Hq + Hkv, hd - 1), (5, Hq, hd - 2)):
+        bad[m, head, e] = float("nan")
+        hit[m, head, e] = True
+        if head < Hq + Hkv and e < rot:                                  # the other element of the pair
+            hit[m, head, e ^ 1 if style == 0 else (e + rot // 2) % rot] = True
+    got = []
+    for x in (clean, bad):
+        cache = R.Cache(torch.zeros(B, Hkv, S, hd), torch.zeros(B, Hkv, S, hd), block_scaled)
+        qf, qh, ql = torch.zeros((B * T, Hq * hd), device=DEV), *(torch.zeros((B * T, Hq * hd), dtype=torch.float16, device=DEV) for _ in range(2))
+        _ops().rope_append_at(x.view(B * T, -1).to(DEV), 1, 0, T, _i32([3, 40]), _i32([2, 20]), _table(rot, 64), style, rot, Hq, Hkv, hd, S, cache.rows[0],
+                              cache.rows[1], q_f32=qf, q_f16=qh, q_f16_lo=ql, **cache.args())
+        got.append(([t.cpu().view(B * T, Hq, hd) for t in (qf, qh, ql)], cache))
+    for a, b in zip(got[0][0], got[1][0]):
+        assert b[hit[:, :Hq]].isnan().all() and torch.equal(a[~hit[:, :Hq]], b[~hit[:, :Hq]])
+    for i, h0 in ((0, Hq), (1, Hq + Hkv)):
+        a, b = (c.values(i) for _, c in got)
+        where = torch.zeros(a.shape, dtype=torch.bool)
+        for m in range(B * T):
+            where[m // T, :, [2, 20][m // T] + m % T] = hit[m, h0:h0 + Hkv]
+        if block_scaled:
+            where = where.any(-1, keepdim=True).expand_as(where)
+        assert b[where].isnan().all() and torch.equal(a[~where], b[~where])
