@@ -230,7 +230,8 @@ int rl_op_logprob_gather(const float *logits, int64_t ld, int32_t M, int32_t V, 
  * not checked; page_size a power of two in [16, 4096], table_stride * page_size >= S); NULL: slabs [B][Hkv][S][hd], page_size and
  * table_stride without effect.  hd is 64 or 128.  weight (fp32) and row_pos / pos (int32) are [B][Hkv][S] arrays beside the cache,
  * indexed by slot whether the cache is paged or not.  Device pointers of q, out, kc, vc and qkv are 16-byte aligned (E_SHAPE
- * otherwise), all others by their element. */
+ * otherwise), all others by their element.  A batch that would need 2^32 threads or more in a launch is refused with E_SHAPE (256 per
+ * appended token, 512 or 1024 per kv head to evict from, 256 per 8192 logits of a row to verify, 128 per split and 8 to 32 query rows of a kv head). */
 
 /* Rotary table with the frequencies scaled for contexts longer than the model was trained on: tab fp32 [n_pos, rot_dim/2, 2] =
  * (cos, sin) of pos * f_r, f_r evaluated in fp64 on the host and copied (synchronously).  rot_dim is the number of leading head

@@ -789,14 +789,26 @@ size_t span_attention_ws_floats(int B, int T, int Hq, int Hkv, int hd, int S, in
     return span_ws(B, T, Hq, Hkv, hd, S, nsplit, weights).total;
 }
 
+// Wavefronts that share a sequence's rows: four where that does not make more workgroups than run at once, two per compute unit (one
+// with 32 query rows), else two: 384 items (48 tokens over 2111 rows) 85.7 us with four, 88.7 with two; 4096 (128 x 5 tokens over 390 rows,
+// 32 heads) 121.6 and 115.4; 512 of 32 query rows (64 x 8 tokens over 1000, 32/8 heads) 46.8 and 42.7.
+static bool span_four_waves(int64_t workgroups, int T, int G) { return workgroups <= (span_rows(T, G) > 16 ? 256 : 512); }
+
+static int span_join_merge_blocks(int B, int T, int Hq, int nsplit) { return nsplit > 1 ? (int)(((int64_t)B * T * Hq + 3) / 4) : 0; }
+// Blocks of 1024 cache rows per (sequence, kv head) whose weights the second kernel adds up.
+static int span_join_key_blocks(int T, int G, int S, int nsplit, bool weights) { return weights && (nsplit > 1 || span_rows(T, G) > 16) ? ceil_div(S, 1024) : 0; }
+
+bool span_attention_grid_fits(int B, int T, int Hq, int Hkv, int S, int nsplit, bool weights) {
+    const int64_t items = (int64_t)B * Hkv * nsplit, row_tiles = span_items(1, T, Hq, Hkv) / Hkv;
+    const int64_t join = span_join_merge_blocks(B, T, Hq, nsplit) + (int64_t)B * Hkv * span_join_key_blocks(T, Hq / Hkv, S, nsplit, weights);
+    return grid_fits(ceil_div64(items, 8) * 8 * row_tiles, span_four_waves(items * row_tiles, T, Hq / Hkv) ? 256 : 128) && grid_fits(join, 256);
+}
+
 template <int HD, int RT, bool I16, bool ONCE>
 static void span_launch(const SpanArgs &a, int row_tiles, hipStream_t st) {
     const int items = a.B * a.Hkv * a.nsplit;
     const unsigned blocks = (unsigned)((int64_t)ceil_div(items, 8) * 8 * row_tiles);
-    // Wavefronts that share a sequence's rows: four where that does not make more workgroups than run at once, two per compute unit (one
-    // with 32 query rows), else two: 384 items (48 tokens over 2111 rows) 85.7 us with four, 88.7 with two; 4096 (128 x 5 tokens over 390 rows,
-    // 32 heads) 121.6 and 115.4; 512 of 32 query rows (64 x 8 tokens over 1000, 32/8 heads) 46.8 and 42.7.
-    const bool four = (int64_t)items * row_tiles <= (RT == 2 ? 256 : 512);
+    const bool four = span_four_waves((int64_t)items * row_tiles, a.T, a.Hq / a.Hkv);
     auto launch = [&](auto wt) {
         constexpr int WT = decltype(wt)::value;
         if (four) span_attention_kernel<HD, RT, 4, I16, ONCE, WT><<<blocks, 256, 0, st>>>(a, row_tiles, items);
@@ -821,9 +833,8 @@ void launch_span_attention(const SpanArgs &a, hipStream_t st) {
     if (a.B <= 0) return;
     if (a.hd == 128) a.map.kscale ? span_launch_tiles<128, true>(a, st) : span_launch_tiles<128, false>(a, st);
     else a.map.kscale ? span_launch_tiles<64, true>(a, st) : span_launch_tiles<64, false>(a, st);
-    const int merge_blocks = a.nsplit > 1 ? (int)(((int64_t)a.B * a.T * a.Hq + 3) / 4) : 0;
-    const bool several = a.nsplit > 1 || span_rows(a.T, a.Hq / a.Hkv) > 16;
-    const int key_blocks = a.weight && several ? ceil_div(a.S, 1024) : 0;
+    const int merge_blocks = span_join_merge_blocks(a.B, a.T, a.Hq, a.nsplit);
+    const int key_blocks = span_join_key_blocks(a.T, a.Hq / a.Hkv, a.S, a.nsplit, a.weight != nullptr);
     const int64_t blocks = merge_blocks + (int64_t)a.B * a.Hkv * key_blocks;
     if (blocks > 0) (a.hd == 128 ? span_join_kernel<128> : span_join_kernel<64>)<<<(unsigned)blocks, 256, 0, st>>>(a, merge_blocks, key_blocks ? key_blocks : 1);
 }

@@ -306,6 +306,8 @@ size_t evict_rows_ws_bytes(int B, int Hkv, int S, int keep) {
     return (size_t)B * Hkv * (2 + 2 * (size_t)(moves < 0 ? 0 : moves)) * sizeof(int32_t);
 }
 
+bool evict_rows_grid_fits(int B, int Hkv, int S) { return grid_fits((int64_t)B * Hkv, S <= 4096 ? 512 : 1024); }
+
 void launch_evict_rows(const EvictArgs &a0, hipStream_t st) {
     EvictArgs a = a0;
     if (a.B <= 0) return;

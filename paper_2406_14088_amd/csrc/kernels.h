@@ -189,6 +189,9 @@ void launch_prefill_attention(const f16_t *q, const f16_t *kc, const f16_t *vc, 
 
 // ---- rope_append_at.hip, attention_span.hip, cache_evict.hip, verify_drafts.hip: steps of several tokens over a bounded cache ----
 // (the operations and the meaning of every argument: rl_gen_ops.h; sizes are checked by the entry points)
+// A launch has fewer than 2^32 threads along an axis; entry points refuse what would need more.
+static inline bool grid_fits(int64_t blocks, int threads) { return blocks * threads <= (int64_t)UINT32_MAX; }
+
 struct RopeAppendAtArgs {
     const float *qkv;
     int nsplit;
@@ -216,6 +219,7 @@ struct SpanArgs {
 };
 int span_attention_splits(int B, int T, int Hq, int Hkv, int hd, int S);  // what nsplit = 0 resolves to
 size_t span_attention_ws_floats(int B, int T, int Hq, int Hkv, int hd, int S, int nsplit, bool weights);
+bool span_attention_grid_fits(int B, int T, int Hq, int Hkv, int S, int nsplit, bool weights);
 void launch_span_attention(const SpanArgs &a, hipStream_t st);
 
 struct EvictArgs {
@@ -232,6 +236,7 @@ struct EvictArgs {
     int B, Hkv, hd, S, keep, recent;
 };
 size_t evict_rows_ws_bytes(int B, int Hkv, int S, int keep);
+bool evict_rows_grid_fits(int B, int Hkv, int S);
 void launch_evict_rows(const EvictArgs &a, hipStream_t st);
 
 struct VerifyArgs {
@@ -249,4 +254,5 @@ struct VerifyArgs {
     void *ws;
 };
 size_t verify_drafts_ws_bytes(int B, int T, int V);
+bool verify_drafts_grid_fits(int B, int T, int V, bool draft);
 void launch_verify_drafts(const VerifyArgs &a, hipStream_t st);

@@ -1758,7 +1758,7 @@ int rl_op_rope_append_at(const float *qkv, int32_t nsplit, size_t split_stride, 
     if (!qkv || !d_pos || !d_slot || !rope_tab || (q_f16_lo && !q_f16)) return RL_GEN_E_NULL;
     RopeAppendAtArgs a;
     if (int rc = span_cache_map(kc, vc, kscale, vscale, table, table_stride, page_size, B, Hkv, hd, S, &a.map)) return rc;
-    if (nsplit < 1 || split_stride % 4 || T <= 0 || (int64_t)B * T > INT32_MAX || tab_rows <= 0 || (rope_style != 0 && rope_style != 1) ||
+    if (nsplit < 1 || split_stride % 4 || T <= 0 || !grid_fits((int64_t)B * T, 256) || tab_rows <= 0 || (rope_style != 0 && rope_style != 1) ||
         rot_dim < 8 || rot_dim > hd || rot_dim % 8 || Hq <= 0 || (int64_t)Hq + 2 * (int64_t)Hkv > 65535)
         return RL_GEN_E_SHAPE;
     if (((uintptr_t)qkv | (uintptr_t)q_f32 | (uintptr_t)q_f16 | (uintptr_t)q_f16_lo | (uintptr_t)rope_tab) % 16) return RL_GEN_E_SHAPE;
@@ -1772,13 +1772,15 @@ int rl_op_rope_append_at(const float *qkv, int32_t nsplit, size_t split_stride, 
     RL_OP_RETURN();
 }
 
-static bool span_shape_ok(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, int32_t S, int32_t nsplit) {
-    return B >= 0 && T > 0 && T <= S && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Hq / Hkv <= 64 && (hd == 64 || hd == 128) && nsplit >= 0 &&
-           nsplit <= 64 && (int64_t)B * T * Hq <= INT32_MAX / 64;
+static bool span_shape_ok(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, int32_t S, int32_t nsplit, bool weights) {
+    if (B < 0 || T <= 0 || T > S || Hq <= 0 || Hkv <= 0 || Hq % Hkv || Hq / Hkv > 64 || (hd != 64 && hd != 128) || nsplit < 0 || nsplit > 64 ||
+        (int64_t)B * T * Hq > INT32_MAX / 64)
+        return false;
+    return span_attention_grid_fits(B, T, Hq, Hkv, S, nsplit ? nsplit : span_attention_splits(B, T, Hq, Hkv, hd, S), weights);
 }
 
 size_t rl_op_span_attention_ws_floats(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, int32_t S, int32_t nsplit, int32_t weights) {
-    if (!span_shape_ok(B, T, Hq, Hkv, hd, S, nsplit)) return 0;
+    if (!span_shape_ok(B, T, Hq, Hkv, hd, S, nsplit, weights != 0)) return 0;
     return span_attention_ws_floats(B, T, Hq, Hkv, hd, S, nsplit ? nsplit : span_attention_splits(B, T, Hq, Hkv, hd, S), weights != 0);
 }
 
@@ -1789,7 +1791,7 @@ int rl_op_span_attention(const float *q, const uint16_t *kc, const uint16_t *vc,
     if (!q || !d_len || !out) return RL_GEN_E_NULL;
     SpanArgs a;
     if (int rc = span_cache_map(kc, vc, kscale, vscale, table, table_stride, page_size, B, Hkv, hd, S, &a.map)) return rc;
-    if (!span_shape_ok(B, T, Hq, Hkv, hd, S, nsplit)) return RL_GEN_E_SHAPE;
+    if (!span_shape_ok(B, T, Hq, Hkv, hd, S, nsplit, weight != nullptr)) return RL_GEN_E_SHAPE;
     if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)out_lo | (uintptr_t)ws) % 16) return RL_GEN_E_SHAPE;
     a.nsplit = nsplit ? nsplit : span_attention_splits(B, T, Hq, Hkv, hd, S);
     const size_t need = span_attention_ws_floats(B, T, Hq, Hkv, hd, S, a.nsplit, weight != nullptr);
@@ -1802,7 +1804,7 @@ int rl_op_span_attention(const float *q, const uint16_t *kc, const uint16_t *vc,
 }
 
 size_t rl_op_evict_rows_ws_bytes(int32_t B, int32_t Hkv, int32_t S, int32_t keep) {
-    if (B < 0 || Hkv <= 0 || S <= 0 || keep < 1 || keep > S) return 0;
+    if (B < 0 || Hkv <= 0 || S <= 0 || keep < 1 || keep > S || !evict_rows_grid_fits(B, Hkv, S)) return 0;
     return evict_rows_ws_bytes(B, Hkv, S, keep);
 }
 
@@ -1813,7 +1815,7 @@ int rl_op_evict_rows(uint16_t *kc, uint16_t *vc, float *kscale, float *vscale, c
     if (!weight || !weight_out || (pos && !pos_out) || !d_len || !ws) return RL_GEN_E_NULL;
     EvictArgs a;
     if (int rc = span_cache_map(kc, vc, kscale, vscale, table, table_stride, page_size, B, Hkv, hd, S, &a.map)) return rc;
-    if (keep < 1 || keep > S || recent < 0 || recent > keep || (uintptr_t)ws % 8) return RL_GEN_E_SHAPE;
+    if (keep < 1 || keep > S || recent < 0 || recent > keep || (uintptr_t)ws % 8 || !evict_rows_grid_fits(B, Hkv, S)) return RL_GEN_E_SHAPE;
     if (ws_bytes < evict_rows_ws_bytes(B, Hkv, S, keep)) return RL_GEN_E_CAPACITY;
     a.kc = kc; a.vc = vc; a.weight = weight; a.weight_out = weight_out; a.pos = pos; a.pos_out = pos ? pos_out : nullptr;
     a.d_len = d_len; a.d_len_out = d_len_out; a.moves = reinterpret_cast<int32_t *>(ws);
@@ -1822,18 +1824,19 @@ int rl_op_evict_rows(uint16_t *kc, uint16_t *vc, float *kscale, float *vscale, c
     RL_OP_RETURN();
 }
 
-static bool verify_shape_ok(int32_t B, int32_t T, int32_t V) {
-    return B >= 0 && T >= 1 && T <= 256 && V > 0 && V <= 1 << 30 && (int64_t)B * (2 * (int64_t)T + 1) * ((V + (int64_t)511) / 512) <= INT32_MAX;
+static bool verify_shape_ok(int32_t B, int32_t T, int32_t V, bool draft) {
+    return B >= 0 && T >= 1 && T <= 256 && V > 0 && V <= 1 << 30 && (int64_t)B * (2 * (int64_t)T + 1) * ((V + (int64_t)511) / 512) <= INT32_MAX &&
+           verify_drafts_grid_fits(B, T, V, draft);
 }
 
-size_t rl_op_verify_drafts_ws_bytes(int32_t B, int32_t T, int32_t V) { return verify_shape_ok(B, T, V) ? verify_drafts_ws_bytes(B, T, V) : 0; }
+size_t rl_op_verify_drafts_ws_bytes(int32_t B, int32_t T, int32_t V) { return verify_shape_ok(B, T, V, false) ? verify_drafts_ws_bytes(B, T, V) : 0; }
 
 int rl_op_verify_drafts(const float *target, int64_t ldt, const float *draft, int64_t ldd, const int32_t *drafts, const float *u,
                         const int32_t *d_span, int32_t B, int32_t T, int32_t V, double temperature, int32_t *accepted, int32_t *tokens,
                         float *logp, void *ws, size_t ws_bytes, void *st) {
     const bool sampled = temperature > 0;
     if (!target || !drafts || !accepted || !tokens || !ws || (sampled && !u)) return RL_GEN_E_NULL;
-    if (!verify_shape_ok(B, T, V) || ldt < V || (sampled && draft && ldd < V) || (uintptr_t)ws % 8) return RL_GEN_E_SHAPE;
+    if (!verify_shape_ok(B, T, V, sampled && draft) || ldt < V || (sampled && draft && ldd < V) || (uintptr_t)ws % 8) return RL_GEN_E_SHAPE;
     if (temperature != temperature || temperature > 1e300 || (sampled && temperature < 1e-30)) return RL_GEN_E_SHAPE;
     if (ws_bytes < verify_drafts_ws_bytes(B, T, V)) return RL_GEN_E_CAPACITY;
     VerifyArgs a;

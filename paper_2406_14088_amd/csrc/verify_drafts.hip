@@ -532,6 +532,11 @@ static int vd_chunk_len(int B, int T, int V) {
 
 size_t verify_drafts_ws_bytes(int B, int T, int V) { return vd_ws(nullptr, B, T, ceil_div(V, vd_chunk_len(B, T, V)), nullptr) + 8; }
 
+bool verify_drafts_grid_fits(int B, int T, int V, bool draft) {
+    const int chunks = ceil_div(V, vd_chunk_len(B, T, V));
+    return grid_fits((int64_t)B * (draft ? 2 * T + 1 : T + 1) * ceil_div(chunks, 4), VD_THREADS) && grid_fits((int64_t)B * chunks, VD_THREADS);
+}
+
 template <int EPT>
 static void vd_launch(const VerifyArgs &a, hipStream_t st) {
     constexpr int LEN = 64 * EPT, PER = LEN / VD_THREADS;

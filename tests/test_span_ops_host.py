@@ -95,3 +95,15 @@ def test_workspace_sizes_of_what_is_refused_are_zero(L):
     assert L.rl_op_evict_rows_ws_bytes(2, 2, 32, 33) == 0 and L.rl_op_evict_rows_ws_bytes(2, 2, 32, 16) > 0
     assert L.rl_op_verify_drafts_ws_bytes(2, 0, 10) == 0 and L.rl_op_verify_drafts_ws_bytes(2, 3, 10) > 0
     assert L.rl_op_evict_rows_ws_bytes(1 << 10, 64, 1 << 20, 1 << 19) > 1 << 32      # sizes beyond 32 bits
+
+
+def test_launches_of_2_to_the_32_threads_are_refused(L):
+    """Where the first kernel of a call cannot be launched the next ones would read what it did not write."""
+    assert _append(L, B=1 << 20, T=16) == E_SHAPE
+    assert _evict(L, B=1 << 22, Hkv=2) == E_SHAPE and _evict(L, B=1 << 21, Hkv=2, S=8192, wsn=1 << 40) == E_SHAPE
+    assert L.rl_op_evict_rows_ws_bytes(1 << 22, 2, 32, 16) == 0 < L.rl_op_evict_rows_ws_bytes((1 << 22) - 1, 2, 32, 16)
+    assert _verify(L, B=9 << 20, T=1, V=10, wsn=1 << 50) == E_SHAPE and _verify(L, B=6 << 20, T=1, V=10, d=P, ldd=10, wsn=1 << 50) == E_SHAPE
+    assert L.rl_op_verify_drafts_ws_bytes(9 << 20, 1, 10) == 0 < L.rl_op_verify_drafts_ws_bytes((8 << 20) - 1, 1, 10)
+    assert _span(L, B=1 << 17, T=1, Hq=16, Hkv=16, S=64, nsplit=16, ws=P, wsn=1 << 50) == E_SHAPE
+    assert _span(L, B=1 << 16, T=32, Hq=8, Hkv=8, S=1 << 16, w=P, ws=P, wsn=1 << 60) == E_SHAPE      # the second kernel's
+    assert L.rl_op_span_attention_ws_floats(1 << 17, 1, 16, 16, 64, 64, 16, 1) == 0 < L.rl_op_span_attention_ws_floats(1 << 17, 1, 16, 16, 64, 64, 15, 1)
