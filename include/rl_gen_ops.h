@@ -267,8 +267,9 @@ int rl_op_rope_append_at(const float *qkv, int32_t nsplit, size_t split_stride, 
  * weight (or NULL): weight[b, h, j] += the sum of p_j over the queries of kv head h and the span's valid tokens -- what
  * rl_op_evict_rows goes by.  Sums are formed in a fixed order (the same bits every time), also those of weight.
  * nsplit: workgroups that share the rows of a sequence, 1 .. 64, or 0: chosen from the shape.  ws: fp32 workspace of ws_floats
- * elements, 16-byte aligned, at least rl_op_span_attention_ws_floats(same arguments, weights = whether weight is given) of them (else
- * RL_GEN_E_CAPACITY; may be NULL when that is 0).
+ * elements, 16-byte aligned.  rl_op_span_attention_ws_floats(same arguments, weights = whether weight is given) are enough for this B and T and every
+ * smaller one, so that a program may size it once for its largest step; a call whose own need is above ws_floats returns RL_GEN_E_CAPACITY
+ * (ws may be NULL for one that needs nothing).  The weights' scores take 4 B T Hq S bytes of it where T Hq / Hkv is a multiple of 32.
  * A query that holds a NaN, or sees a row whose K or V does, gives NaN in out and out_lo (from q or K: also in weight); a block-scaled row counts as one
  * whose scale is not finite.  An infinite half in V gives NaN or the largest half of its sign, one in K a score that is infinite or NaN.  Rows that a
  * query does not see never reach its result, whatever they hold.  q times log2(e) / sqrt(hd) saturates at +-131008, out and out_lo at
@@ -312,7 +313,8 @@ size_t rl_op_evict_rows_ws_bytes(int32_t B, int32_t Hkv, int32_t S, int32_t keep
  * NaN where that row's largest logit is not finite), 0 for -1.
  * Weights and sums are formed in fp64 from the fp32 logits (relative error below 1e-11), in a fixed order.  1 <= T <= 256,
  * 1 <= V <= 2^30.
- * ws: DEVICE, ws_bytes long, 8-byte aligned, at least rl_op_verify_drafts_ws_bytes (else RL_GEN_E_CAPACITY). */
+ * ws: DEVICE, ws_bytes long, 8-byte aligned.  rl_op_verify_drafts_ws_bytes are enough for this B and T and every smaller one; a call whose own need
+ * is above ws_bytes returns RL_GEN_E_CAPACITY. */
 int rl_op_verify_drafts(const float *target, int64_t ldt, const float *draft, int64_t ldd, const int32_t *drafts, const float *u,
                         const int32_t *d_span, int32_t B, int32_t T, int32_t V, double temperature, int32_t *accepted, int32_t *tokens,
                         float *logp, void *ws, size_t ws_bytes, void *hip_stream);

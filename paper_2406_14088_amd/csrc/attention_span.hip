@@ -789,6 +789,19 @@ size_t span_attention_ws_floats(int B, int T, int Hq, int Hkv, int hd, int S, in
     return span_ws(B, T, Hq, Hkv, hd, S, nsplit, weights).total;
 }
 
+// With nsplit given, need grows with B and T.  Chosen from the shape, splits appear as a batch shrinks: b sequences of t tokens in k workgroups
+// per kv head take s <= 256 / (b Hkv k) of them, so b t Hq s = b Hkv k s (t G / k) is at most 256 rows of a workgroup, min(t G, 32).
+size_t span_attention_ws_floats_up_to(int B, int T, int Hq, int Hkv, int hd, int S, int nsplit, bool weights) {
+    const int most = nsplit || B == 0 ? 1 : span_attention_splits(1, 1, Hq, Hkv, hd, S);
+    if (most <= 1) return span_ws(B, T, Hq, Hkv, hd, S, nsplit ? nsplit : 1, weights).total;
+    const int64_t rows = (int64_t)B * T * Hq, tg = (int64_t)T * (Hq / Hkv);
+    int64_t parts = 256 * (tg < 32 ? tg : 32);
+    parts = parts < rows * most ? parts : rows * most;
+    parts = parts > rows ? parts : rows;
+    const SpanWs one = span_ws(B, T, Hq, Hkv, hd, S, 1, weights);
+    return (size_t)(parts * 2 + 3) / 4 * 4 + (size_t)parts * hd + (one.total - one.scores);
+}
+
 // Wavefronts that share a sequence's rows: four where that does not make more workgroups than run at once, two per compute unit (one
 // with 32 query rows), else two: 384 items (48 tokens over 2111 rows) 85.7 us with four, 88.7 with two; 4096 (128 x 5 tokens over 390 rows,
 // 32 heads) 121.6 and 115.4; 512 of 32 query rows (64 x 8 tokens over 1000, 32/8 heads) 46.8 and 42.7.

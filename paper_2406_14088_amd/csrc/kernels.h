@@ -219,6 +219,7 @@ struct SpanArgs {
 };
 int span_attention_splits(int B, int T, int Hq, int Hkv, int hd, int S);  // what nsplit = 0 resolves to
 size_t span_attention_ws_floats(int B, int T, int Hq, int Hkv, int hd, int S, int nsplit, bool weights);
+size_t span_attention_ws_floats_up_to(int B, int T, int Hq, int Hkv, int hd, int S, int nsplit, bool weights);  // of this and any smaller B and T
 bool span_attention_grid_fits(int B, int T, int Hq, int Hkv, int S, int nsplit, bool weights);
 void launch_span_attention(const SpanArgs &a, hipStream_t st);
 
@@ -254,5 +255,6 @@ struct VerifyArgs {
     void *ws;
 };
 size_t verify_drafts_ws_bytes(int B, int T, int V);
+size_t verify_drafts_ws_bytes_up_to(int B, int T, int V);  // of this and any smaller B and T
 bool verify_drafts_grid_fits(int B, int T, int V, bool draft);
 void launch_verify_drafts(const VerifyArgs &a, hipStream_t st);

@@ -1781,7 +1781,7 @@ static bool span_shape_ok(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t
 
 size_t rl_op_span_attention_ws_floats(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t hd, int32_t S, int32_t nsplit, int32_t weights) {
     if (!span_shape_ok(B, T, Hq, Hkv, hd, S, nsplit, weights != 0)) return 0;
-    return span_attention_ws_floats(B, T, Hq, Hkv, hd, S, nsplit ? nsplit : span_attention_splits(B, T, Hq, Hkv, hd, S), weights != 0);
+    return span_attention_ws_floats_up_to(B, T, Hq, Hkv, hd, S, nsplit, weights != 0);
 }
 
 int rl_op_span_attention(const float *q, const uint16_t *kc, const uint16_t *vc, const float *kscale, const float *vscale,
@@ -1829,7 +1829,7 @@ static bool verify_shape_ok(int32_t B, int32_t T, int32_t V, bool draft) {
            verify_drafts_grid_fits(B, T, V, draft);
 }
 
-size_t rl_op_verify_drafts_ws_bytes(int32_t B, int32_t T, int32_t V) { return verify_shape_ok(B, T, V, false) ? verify_drafts_ws_bytes(B, T, V) : 0; }
+size_t rl_op_verify_drafts_ws_bytes(int32_t B, int32_t T, int32_t V) { return verify_shape_ok(B, T, V, false) ? verify_drafts_ws_bytes_up_to(B, T, V) : 0; }
 
 int rl_op_verify_drafts(const float *target, int64_t ldt, const float *draft, int64_t ldd, const int32_t *drafts, const float *u,
                         const int32_t *d_span, int32_t B, int32_t T, int32_t V, double temperature, int32_t *accepted, int32_t *tokens,

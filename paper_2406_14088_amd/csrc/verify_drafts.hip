@@ -532,6 +532,19 @@ static int vd_chunk_len(int B, int T, int V) {
 
 size_t verify_drafts_ws_bytes(int B, int T, int V) { return vd_ws(nullptr, B, T, ceil_div(V, vd_chunk_len(B, T, V)), nullptr) + 8; }
 
+// Chunks of 512 appear as a batch shrinks: for every number of tokens, the largest batch that takes them.
+size_t verify_drafts_ws_bytes_up_to(int B, int T, int V) {
+    size_t most = vd_ws(nullptr, B, T, ceil_div(V, 2048), nullptr) + 8;
+    for (int t = 1; t <= T; ++t) {
+        const int64_t per = (int64_t)(t + 1) * ceil_div(V, 2048);
+        const int b = (int)(1023 / per < B ? 1023 / per : B);
+        if (b < 1) break;
+        const size_t n = verify_drafts_ws_bytes(b, t, V);
+        most = n > most ? n : most;
+    }
+    return most;
+}
+
 bool verify_drafts_grid_fits(int B, int T, int V, bool draft) {
     const int chunks = ceil_div(V, vd_chunk_len(B, T, V));
     return grid_fits((int64_t)B * (draft ? 2 * T + 1 : T + 1) * ceil_div(chunks, 4), VD_THREADS) && grid_fits((int64_t)B * chunks, VD_THREADS);

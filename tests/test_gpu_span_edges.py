@@ -42,3 +42,34 @@ def test_append_keeps_not_a_number(block_scaled, hd, rot, style):
         if block_scaled:
             where = where.any(-1, keepdim=True).expand_as(where)
         assert b[where].isnan().all() and torch.equal(a[~where], b[~where])
+
+
+def test_workspaces_of_a_large_batch_serve_every_smaller_one():
+    ops = _ops()
+    V, B, T = 32000, 40, 6
+    g = torch.Generator().manual_seed(1)
+    logits = torch.randn((B * (T + 1), V), generator=g).to(DEV)
+    drafts, u = torch.randint(0, V, (B, T), generator=g, dtype=torch.int32).to(DEV), torch.rand((B, T + 1), generator=g).to(DEV)
+    ws = torch.empty(ops.verify_drafts_ws_bytes(B, T, V), dtype=torch.uint8, device=DEV)
+    for b in (40, 33, 17, 11, 10, 9, 5, 1):
+        for t in (6, 5, 2, 1):
+            outs = []
+            for w in (ws, torch.empty(ops.verify_drafts_ws_bytes(b, t, V), dtype=torch.uint8, device=DEV)):
+                acc, tok = torch.zeros(b, dtype=torch.int32, device=DEV), torch.zeros((b, t + 1), dtype=torch.int32, device=DEV)
+                ops.verify_drafts(logits[: b * (t + 1)], drafts[:b, :t].contiguous(), u[:b, : t + 1].contiguous(), acc, tok, w, 1.0, draft=logits[:b * t] * 0.9)
+                outs.append((acc, tok))
+            assert all(torch.equal(x, y) for x, y in zip(*outs))
+    B, T, Hq, Hkv, hd, S = 48, 12, 16, 4, 64, 2048
+    k, v = torch.randn((2, B, Hkv, S, hd), generator=g).to(torch.float16).to(DEV)
+    q = torch.randn((B * T, Hq * hd), generator=g).to(DEV)
+    for weights in (False, True):
+        ws = torch.empty(ops.span_attention_ws_floats(B, T, Hq, Hkv, hd, S, 0, weights), device=DEV)
+        for b in (48, 33, 32, 16, 7, 2, 1):
+            for t in (12, 8, 5, 4, 2, 1):
+                lens = torch.randint(0, S - t, (b,), generator=g, dtype=torch.int32).to(DEV)
+                outs = []
+                for w in (ws, torch.empty(ops.span_attention_ws_floats(b, t, Hq, Hkv, hd, S, 0, weights), device=DEV)):
+                    out, weight = torch.zeros((b * t, Hq * hd), dtype=torch.float16, device=DEV), torch.zeros((b, Hkv, S), device=DEV)
+                    ops.span_attention(q[: b * t], k, v, lens, out, w, t, Hq, Hkv, hd, S, weight=weight if weights else None)
+                    outs.append((out, weight))
+                assert all(torch.equal(x, y) for x, y in zip(*outs))

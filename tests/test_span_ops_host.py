@@ -107,3 +107,24 @@ def test_launches_of_2_to_the_32_threads_are_refused(L):
     assert _span(L, B=1 << 17, T=1, Hq=16, Hkv=16, S=64, nsplit=16, ws=P, wsn=1 << 50) == E_SHAPE
     assert _span(L, B=1 << 16, T=32, Hq=8, Hkv=8, S=1 << 16, w=P, ws=P, wsn=1 << 60) == E_SHAPE      # the second kernel's
     assert L.rl_op_span_attention_ws_floats(1 << 17, 1, 16, 16, 64, 64, 16, 1) == 0 < L.rl_op_span_attention_ws_floats(1 << 17, 1, 16, 16, 64, 64, 15, 1)
+
+
+def test_a_workspace_for_the_largest_step_serves_smaller_ones(L):
+    """A generation loop sizes its workspaces once, and its batch shrinks as sequences end."""
+    for V in (10, 1024, 32000, 128256, 600000):
+        for T in (1, 3, 5, 16, 40):
+            sizes = [L.rl_op_verify_drafts_ws_bytes(B, T, V) for B in range(0, 70)]
+            assert sizes == sorted(sizes), (V, T)
+        sizes = [L.rl_op_verify_drafts_ws_bytes(12, T, V) for T in range(1, 257)]
+        assert sizes == sorted(sizes), V
+    for weights in (0, 1):
+        for nsplit in (0, 1, 3):
+            for Hq, Hkv, hd in ((32, 8, 128), (32, 32, 128), (64, 8, 64), (7, 1, 64), (600, 300, 64)):
+                for S in (100, 600, 4096, 100000):
+                    for T in (1, 2, 4, 8, 9, 33):
+                        sizes = [L.rl_op_span_attention_ws_floats(B, T, Hq, Hkv, hd, S, nsplit, weights) for B in range(0, 70)]
+                        assert sizes == sorted(sizes), (weights, nsplit, Hq, Hkv, hd, S, T)
+                    sizes = [L.rl_op_span_attention_ws_floats(5, T, Hq, Hkv, hd, S, nsplit, weights) for T in range(1, 100)]
+                    assert sizes == sorted(sizes), (weights, nsplit, Hq, Hkv, hd, S)
+    sizes = [L.rl_op_evict_rows_ws_bytes(B, 8, 2112, 2048) for B in range(70)]
+    assert sizes == sorted(sizes)
