@@ -199,7 +199,8 @@ def _stream() -> int:
 
 class _Fit:
     """Operands of the span operators: all on the current GPU, contiguous, of one of the element types and long enough, so that no kernel
-    reads or writes outside them.  Calling it gives the pointer (None for None)."""
+    reads or writes outside them, whatever the sizes given (ctypes cuts numbers off at 32 bits).  Calling it gives the pointer (None for
+    None).  Of a pool of pages only the owner knows the length that page lists may reach: K, V and scales have to agree in it."""
 
     __slots__ = ("where", "dev")
     f32 = i32 = h16 = raw = None      # element types
@@ -214,7 +215,7 @@ class _Fit:
     def __call__(self, name: str, t, types, n: int):
         if t is None:
             return None
-        if t.dtype in types and t.get_device() == self.dev and t.numel() >= n and t.is_contiguous():
+        if t.dtype in types and t.get_device() == self.dev and 0 <= n <= t.numel() and t.is_contiguous():
             return t.data_ptr()
         raise RlGenError(-2, self.where, f"{name}: expected a contiguous tensor of at least {n} elements of {types[0]} on the current GPU "
                                          f"(cuda:{self.dev}), got {t.numel()} of {t.dtype} on {t.device}")
@@ -229,9 +230,17 @@ class _Fit:
         if table is not None:
             if table.dim() != 2 or table.shape[0] < B:
                 raise RlGenError(-2, self.where, "table: expected int32 [B, pages per sequence]")
-            rows, pages, stride = 0, self("table", table, _Fit.i32, 0), table.shape[1]
+            if S >> 31:
+                raise RlGenError(-2, self.where, f"S = {S}")
+            rows, pages, stride = self.need("kc", kc).numel() // max(hd, 1), self("table", table, _Fit.i32, 0), table.shape[1]
         return (self("kc", kc, _Fit.h16, rows * hd), self("vc", vc, _Fit.h16, rows * hd), self("kscale", kscale, _Fit.f32, rows),
                 self("vscale", vscale, _Fit.f32, rows), pages, stride)
+
+    def need(self, name: str, t):
+        """t, which a size is taken from."""
+        if t is None:
+            raise RlGenError(-1, self.where, name)
+        return t
 
     def check(self, rc: int):
         if rc != 0:
@@ -628,14 +637,16 @@ class _Ops:
         int32 [B]."""
         fit = _Fit("rl_op_rope_append_at")
         f32, i32, h16 = fit.f32, fit.i32, fit.h16
-        B = d_pos.numel()
+        B = fit.need("d_pos", d_pos).numel()
         if B == 0:
             return
         n, side = B * T * Hq * hd, B * Hkv * S
         k, v, ks, vs, pages, stride = fit.cache(kc, vc, kscale, vscale, table, B, Hkv, hd, S)
+        if split_stride < 0:
+            raise RlGenError(-2, fit.where, f"split_stride = {split_stride}")
         fit.check(lib().rl_op_rope_append_at(fit("qkv", qkv, f32, (nsplit - 1) * split_stride + B * T * (Hq + 2 * Hkv) * hd), nsplit, split_stride,
                                              B, T, fit("d_pos", d_pos, i32, B), fit("d_slot", d_slot, i32, B), fit("d_span", d_span, i32, B),
-                                             fit("rope_tab", rope_tab, f32, rot_dim), rope_tab.numel() // max(rot_dim, 1), rope_style, rot_dim, Hq, Hkv,
+                                             fit("rope_tab", fit.need("rope_tab", rope_tab), f32, rot_dim), rope_tab.numel() // max(rot_dim, 1), rope_style, rot_dim, Hq, Hkv,
                                              hd, S, fit("q_f32", q_f32, f32, n), fit("q_f16", q_f16, h16, n), fit("q_f16_lo", q_f16_lo, h16, n), k, v,
                                              ks, vs, pages, stride, page_size, fit("weight", weight, f32, side), fit("row_pos", row_pos, i32, side),
                                              fit.stream()))
@@ -649,7 +660,7 @@ class _Ops:
         added to."""
         fit = _Fit("rl_op_span_attention")
         f32, i32, h16 = fit.f32, fit.i32, fit.h16
-        B = d_len.numel()
+        B = fit.need("d_len", d_len).numel()
         if B == 0:
             return
         n = B * T * Hq * hd
@@ -667,15 +678,17 @@ class _Ops:
         """weight / pos [B, Hkv, S]; d_len int32 [B]; ws: evict_rows_ws_bytes(...) bytes; d_len_out may be None."""
         fit = _Fit("rl_op_evict_rows")
         f32, i32 = fit.f32, fit.i32
-        B = d_len.numel()
+        B = fit.need("d_len", d_len).numel()
         if B == 0:
             return
+        if (keep | recent) >> 31:
+            raise RlGenError(-2, fit.where, f"keep = {keep}, recent = {recent}")
         side = B * Hkv * S
         k, v, ks, vs, pages, stride = fit.cache(kc, vc, kscale, vscale, table, B, Hkv, hd, S)
         fit.check(lib().rl_op_evict_rows(k, v, ks, vs, pages, stride, page_size, fit("weight", weight, f32, side),
                                          fit("weight_out", weight_out, f32, side), fit("pos", pos, i32, side), fit("pos_out", pos_out, i32, side),
                                          fit("d_len", d_len, i32, B), fit("d_len_out", d_len_out, i32, B), fit("ws", ws, fit.raw, 0),
-                                         ws.numel() * ws.element_size(), B, Hkv, hd, S, keep, recent, fit.stream()))
+                                         0 if ws is None else ws.numel() * ws.element_size(), B, Hkv, hd, S, keep, recent, fit.stream()))
 
     def verify_drafts_ws_bytes(self, B, T, V):
         return int(lib().rl_op_verify_drafts_ws_bytes(B, T, V))
@@ -685,6 +698,8 @@ class _Ops:
         [B, T+1] (None when temperature <= 0); accepted int32 [B]; tokens int32, logp fp32 [B, T+1]; ws: verify_drafts_ws_bytes(...)."""
         fit = _Fit("rl_op_verify_drafts")
         f32, i32 = fit.f32, fit.i32
+        if fit.need("drafts", drafts).dim() != 2 or fit.need("target", target).dim() != 2:
+            raise RlGenError(-2, fit.where, "drafts: expected int32 [B, T], target: fp32 [B * (T + 1), V]")
         B, T = drafts.shape
         if B == 0:
             return
@@ -703,7 +718,7 @@ class _Ops:
         fit.check(lib().rl_op_verify_drafts(tp, ldt, dp, ldd, fit("drafts", drafts, i32, B * T), fit("u", u, f32, B * (T + 1)),
                                             fit("d_span", d_span, i32, B), B, T, V, float(temperature), fit("accepted", accepted, i32, B),
                                             fit("tokens", tokens, i32, B * (T + 1)), fit("logp", logp, f32, B * (T + 1)), fit("ws", ws, fit.raw, 0),
-                                            ws.numel() * ws.element_size(), fit.stream()))
+                                            0 if ws is None else ws.numel() * ws.element_size(), fit.stream()))
 
     def sample(self, logits, temperature, u, nxt):
         B, V = logits.shape

@@ -128,3 +128,9 @@ def test_a_workspace_for_the_largest_step_serves_smaller_ones(L):
                     assert sizes == sorted(sizes), (weights, nsplit, Hq, Hkv, hd, S)
     sizes = [L.rl_op_evict_rows_ws_bytes(B, 8, 2112, 2048) for B in range(70)]
     assert sizes == sorted(sizes)
+
+
+def test_partials_that_lie_nowhere_are_refused(L):
+    """A negative distance of partials, as a size, would be read in front of the operand."""
+    for stride in (2 ** 64 - 4, 2 ** 64 - 4096, 2 ** 63, 2 ** 61):
+        assert _append(L, nsplit=2, stride=stride) == E_SHAPE
