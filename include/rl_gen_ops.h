@@ -270,9 +270,9 @@ int rl_op_rope_append_at(const float *qkv, int32_t nsplit, size_t split_stride, 
  * elements, 16-byte aligned.  rl_op_span_attention_ws_floats(same arguments, weights = whether weight is given) are enough for this B and T and every
  * smaller one, so that a program may size it once for its largest step; a call whose own need is above ws_floats returns RL_GEN_E_CAPACITY
  * (ws may be NULL for one that needs nothing).  The weights' scores take 4 B T Hq S bytes of it where T Hq / Hkv is a multiple of 32.
- * A query that holds a NaN, or sees a row whose K or V does, gives NaN in out and out_lo (from q or K: also in weight); a block-scaled row counts as one
+ * A query that holds a NaN or an infinity, or sees a row whose K or V holds a NaN, gives NaN in out and out_lo (from q or K: also in weight); a block-scaled row counts as one
  * whose scale is not finite.  An infinite half in V gives NaN or the largest half of its sign, one in K a score that is infinite or NaN.  Rows that a
- * query does not see never reach its result, whatever they hold.  q times log2(e) / sqrt(hd) saturates at +-131008, out and out_lo at
+ * query does not see never reach its result, whatever they hold.  Finite q times log2(e) / sqrt(hd) saturates at +-131008, out and out_lo at
  * +-65504.  Hq/Hkv <= 64. */
 int rl_op_span_attention(const float *q, const uint16_t *kc, const uint16_t *vc, const float *kscale, const float *vscale,
                          const int32_t *table, int32_t table_stride, int32_t page_size, const int32_t *d_len, const int32_t *d_span,

@@ -204,13 +204,14 @@ class _Fit:
 
     __slots__ = ("where", "dev")
     f32 = i32 = h16 = raw = None      # element types
+    torch_c = None
 
     def __init__(self, where: str):
-        import torch
         if _Fit.f32 is None:
+            import torch
             _Fit.i32, _Fit.h16 = (torch.int32,), (torch.float16, torch.int16, torch.uint16)
-            _Fit.raw, _Fit.f32 = (torch.uint8, torch.int64, torch.int32, torch.float32), (torch.float32,)
-        self.where, self.dev = where, torch._C._cuda_getDevice()
+            _Fit.raw, _Fit.f32, _Fit.torch_c = (torch.uint8, torch.int64, torch.int32, torch.float32), (torch.float32,), torch._C
+        self.where, self.dev = where, _Fit.torch_c._cuda_getDevice()
 
     def __call__(self, name: str, t, types, n: int):
         if t is None:
@@ -221,8 +222,7 @@ class _Fit:
                                          f"(cuda:{self.dev}), got {t.numel()} of {t.dtype} on {t.device}")
 
     def stream(self) -> int:
-        import torch
-        return torch._C._cuda_getCurrentRawStream(self.dev)
+        return _Fit.torch_c._cuda_getCurrentRawStream(self.dev)
 
     def cache(self, kc, vc, kscale, vscale, table, B: int, Hkv: int, hd: int, S: int):
         """Pointers of kc, vc, kscale, vscale, table and the stride of the page lists."""

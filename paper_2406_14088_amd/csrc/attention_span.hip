@@ -277,7 +277,6 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
     // ---- Q^T operands: column c of tile nt = query row r0 + TR nt + c % TR; k-step s covers elements 32 s + 8 j + 0..7
     f16x8_t qf[NT][KS], ql[RT ? NT : 1][RT ? KS : 1];
     const float qscale = rsqrtf((float)HD) * 1.44269504f;
-    float finite = 0.f;                           // NaN once an element is not
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -286,20 +285,11 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
             for (int e = 0; e < 8; ++e) {
                 const float v = row_ok[nt] ? qraw[nt][2 * s + (e >> 2)][e & 3] * qscale : 0.f;
                 const _Float16 hi = (_Float16)__builtin_amdgcn_fmed3f(v, -65504.f, 65504.f);  // saturating, like every half here
-                const _Float16 lo = (_Float16)__builtin_amdgcn_fmed3f(v - (float)hi, -65504.f, 65504.f);
+                // v * 0: the limits take a NaN for the lower one, an infinity for the upper; the low term is a NaN then
+                const _Float16 lo = (_Float16)__builtin_fmaf(v, 0.f, __builtin_amdgcn_fmed3f(v - (float)hi, -65504.f, 65504.f));
                 qf[nt][s][e] = RT || c < 8 ? hi : lo;
                 if (RT) ql[RT ? nt : 0][RT ? s : 0][e] = lo;
-                finite = __builtin_fmaf(v, 0.f, finite);
             }
-    if (__any(finite != 0.f)) {                   // rare, and kept out of the way of the first tile: the limits above take a NaN for the lower one
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (row_ok[nt] && qraw[nt][2 * s + (e >> 2)][e & 3] != qraw[nt][2 * s + (e >> 2)][e & 3]) qf[nt][s][e] = (_Float16)__builtin_nanf("");
-    }
 
     int vaddr[OT], kaddr[KL ? KS : 1];
 #pragma unroll
@@ -596,12 +586,13 @@ __global__ __launch_bounds__(64 * W, RT == 2 ? 1 : 2) void span_attention_kernel
             const size_t at = (((size_t)b * a.T + rr / G) * a.Hq + kvh * G + rr % G) * HD + e0;
             u32x4_t h, l;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                h[e] = pack_f16x2_nan(o[2 * e] * inv, o[2 * e + 1] * inv);
-                l[e] = pack_f16x2_lo_nan(o[2 * e] * inv, o[2 * e + 1] * inv, h[e]);
-            }
+            for (int e = 0; e < 4; ++e) h[e] = pack_f16x2_nan(o[2 * e] * inv, o[2 * e + 1] * inv);
             *reinterpret_cast<u32x4_t *>(a.out + at) = h;
-            if (a.out_lo) *reinterpret_cast<u32x4_t *>(a.out_lo + at) = l;
+            if (a.out_lo) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) l[e] = pack_f16x2_lo_nan(o[2 * e] * inv, o[2 * e + 1] * inv, h[e]);
+                *reinterpret_cast<u32x4_t *>(a.out_lo + at) = l;
+            }
         }
     }
     if (WT == 2) {

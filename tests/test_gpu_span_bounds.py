@@ -87,9 +87,11 @@ def test_not_a_number_comes_out_as_one(T, Hq, Hkv, nsplit, block_scaled):
     bad[0, T - 1, 2, 5] = float("nan")
     hit = torch.zeros((2, T, Hq), dtype=torch.bool)
     hit[0, T - 1, 2] = True
-    for name, at in (("q", 0), ("k", 40), ("v", 40), ("k", n + T - 1), ("v", n + T - 1)):
+    for name, at in (("q", 0), ("inf", 0), ("k", 40), ("v", 40), ("k", n + T - 1), ("v", n + T - 1)):
         cache = R.Cache(k, v, block_scaled)
-        if name != "q":
+        if name == "inf":
+            bad[0, T - 1, 2, 5] = -float("inf")
+        if name in "kv":
             i = "kv".index(name)
             if block_scaled:
                 cache.scales[i][0, 0, at] = float("nan")
@@ -97,7 +99,7 @@ def test_not_a_number_comes_out_as_one(T, Hq, Hkv, nsplit, block_scaled):
                 cache.rows[i][0, 0, at] = float("nan")
             hit = torch.zeros((2, T, Hq), dtype=torch.bool)
             hit[0, max(0, at - n):] = True
-        out, lo = _run_span(cache, bad if name == "q" else q, [n, n - 9], T, nsplit)
+        out, lo = _run_span(cache, q if name in "kv" else bad, [n, n - 9], T, nsplit)
         assert out[hit].isnan().all() and lo[hit].isnan().all(), (name, at)
         assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lo[~hit], clean_lo[~hit]), (name, at)
 
