@@ -124,3 +124,45 @@ def test_an_infinite_value_is_no_finite_result(block_scaled):
                 cache = R.Cache(k, v, True)
                 cache.scales[0][0, 0, at] = sign * float("inf")
                 assert _run_span(cache, q, [n], T)[0][0, max(0, at - n):].isnan().all()
+
+
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("nsplit", [2, 5, 64])
+@pytest.mark.parametrize("block_scaled,page", [(False, 0), (True, 16)])
+@pytest.mark.parametrize("T,Hq,Hkv,hd", [(1, 4, 2, 128), (2, 8, 2, 64), (3, 8, 2, 128), (6, 8, 2, 64), (8, 4, 1, 128), (11, 8, 1, 64)])
+def test_splits_of_every_number_of_query_rows(T, Hq, Hkv, hd, block_scaled, page, nsplit, weights):
+    """2, 8, 12, 24, 32 and 88 query rows of a kv head (three workgroups), the rows of a sequence on several workgroups."""
+    B, S = 3, 432
+    g = torch.Generator().manual_seed(T + nsplit)
+    cache = R.Cache(_rnd(g, B, Hkv, S, hd), _rnd(g, B, Hkv, S, hd), block_scaled, page)
+    _check(cache, _rnd(g, B, T, Hq, hd, std=1.5), [S - T, 0, 130], T, nsplit, [T, T, max(1, T - 1)], weights)
+
+
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("block_scaled", [False, True])
+@pytest.mark.parametrize("T,Hq", [(2, 4), (3, 4), (6, 4)])
+def test_page_lists_longer_than_a_wavefront(T, Hq, block_scaled, weights):
+    """A wavefront's share of 16-row pages passes 64, 128 and 192 entries of its list; lengths that end just behind a refill."""
+    B, hd, S, page = 4, 64, 13120, 16
+    g = torch.Generator().manual_seed(T)
+    cache = R.Cache(_rnd(g, B, 1, S, hd), _rnd(g, B, 1, S, hd), block_scaled, page)
+    _check(cache, _rnd(g, B, T, Hq, hd), [S - T, 4 * 1024 + 1, 4097 + 128, 8 * 1024 + 17], T, 1, None, weights)
+
+
+@pytest.mark.parametrize("nsplit", [0, 1, 4])
+@pytest.mark.parametrize("block_scaled,page", [(False, 64), (True, 0)])
+def test_a_chunk_of_a_prompt_over_a_cached_prefix(block_scaled, page, nsplit):
+    B, T, Hq, Hkv, hd, S = 2, 70, 8, 2, 128, 640
+    g = torch.Generator().manual_seed(nsplit)
+    cache = R.Cache(_rnd(g, B, Hkv, S, hd), _rnd(g, B, Hkv, S, hd), block_scaled, page)
+    _check(cache, _rnd(g, B, T, Hq, hd), [S - T, 37], T, nsplit, [T, 51])
+
+
+@pytest.mark.parametrize("block_scaled", [False, True])
+@pytest.mark.parametrize("T,Hq,Hkv,hd", [(1, 4, 4, 64), (2, 16, 2, 128), (5, 8, 2, 128), (9, 16, 4, 64)])
+def test_each_result_within_its_own_bound(T, Hq, Hkv, hd, block_scaled):
+    """Ordinary rows: the second half terms of queries, probabilities and integer rows decide whether this holds."""
+    for n in (3, 40, 300):
+        g = torch.Generator().manual_seed(n + T)
+        k, v = _rnd(g, 1, Hkv, n + T, hd), _rnd(g, 1, Hkv, n + T, hd)
+        _check(R.Cache(k, v, block_scaled), _rnd(g, 1, T, Hq, hd, std=1.5), [n], T)

@@ -5,7 +5,7 @@ import torch
 
 from tests.gpu_util import DEV
 from tests import ref_span as R
-from tests.test_gpu_span_ops import _i32, _ops, _rnd, _table
+from tests.test_gpu_span_ops import _check_verify, _drafting, _i32, _ops, _rnd, _table
 
 pytestmark = pytest.mark.gpu
 
@@ -107,3 +107,32 @@ def test_operands_that_are_missing_or_do_not_belong_together():
                 fn(**{**good, **change})
                 print("not refused:", fn.__name__, change)
     torch.cuda.synchronize()
+
+
+# ---------------------------------------------------------------------------------------------- draft verification, long paths
+def _drawn(u, where):
+    """u whose last entry puts the draw near the start, the middle or the end of what is left to draw from."""
+    u = u.clone()
+    u[:, -1] = {"first": 1e-4, "middle": 0.5, "last": 1 - 2.0 ** -24}[where]
+    return u
+
+
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+@pytest.mark.parametrize("form", ["sampled", "onehot", "greedy"])
+@pytest.mark.parametrize("B,T,V", [(14, 4, 32000), (1, 1, 128256), (2, 3, 131073), (1, 5, 300001), (33, 1, 32003), (3, 200, 67), (2, 256, 300), (520, 1, 4000)])
+def test_verify_drafts_long_paths(B, T, V, form, where):
+    """Chunks of 2048 logits (14 x 5 rows of 32000, 131073, 300001 and 520 x 2 of 4000), more than 64 chunks to join (128256: 251 of 512; 131073
+    and 300001: 65 and 147 of 2048), more drafted tokens than the wavefronts that put them out (200, 256)."""
+    t, d, drafts, u = _drafting(B, T, V, V + T, spread=1.0 if V < 1000 else 2.5, apart=0.1 if T > 100 else 0.6, heat=0.02 if form == "greedy" else 0.8)
+    u = _drawn(u, where)
+    if T > 100:          # most drafts are accepted, a sequence ends late or at its end
+        u[:, :-1] *= 0.5
+        if form != "sampled":
+            drafts = t[:, :T].argmax(-1)
+            drafts[0, T - 7] = (drafts[0, T - 7] + 1) % V
+            u[:, :-1] *= 1e-3
+    elif B > 1:          # rejected at once, later, not at all
+        u[0, 0], u[-1, :T] = 1 - 2.0 ** -24, 0.0
+    acc = _check_verify(t, None if form == "onehot" else d, drafts, u, 0.0 if form == "greedy" else 0.8, span=None if where == "middle" else [T - i % 2 * (T > 1) for i in range(B)])
+    if T > 100:
+        assert max(acc) > 192
