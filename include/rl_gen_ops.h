@@ -253,7 +253,7 @@ int rl_op_build_rope_table_scaled(float *tab, int32_t n_pos, int32_t rot_dim, fl
  * q goes to q_f32 and / or q_f16 (+ q_f16_lo, its second half term), each [B*T, Hq*hd] or NULL; k and v become cache rows.
  * weight and row_pos (either may be NULL): the entry of every new row is set to 0 and to its position.
  * A row whose position is outside [0, tab_rows) or whose slot is outside [0, S) is skipped whole.  Halves saturate at +-65504, a NaN stays one;
- * a block-scaled row that holds one gets a scale that is NaN. */
+ * a block-scaled row that holds one gets a scale that is NaN, one whose largest magnitude is not above 2^-100 becomes zeros. */
 int rl_op_rope_append_at(const float *qkv, int32_t nsplit, size_t split_stride, int32_t B, int32_t T, const int32_t *d_pos,
                          const int32_t *d_slot, const int32_t *d_span, const float *rope_tab, int32_t tab_rows, int32_t rope_style,
                          int32_t rot_dim, int32_t Hq, int32_t Hkv, int32_t hd, int32_t S, float *q_f32, uint16_t *q_f16, uint16_t *q_f16_lo,

@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256) void rope_append_at_kernel(RopeAppendAtArgs a)
     f16_t *dst = (kind == 1 ? a.kc : a.vc) + rowi * hd;
     u32x2_t hx, hy;
     if (SCALED) {
-        const float inv = kv_inv_of(am);
+        const float inv = am > 0x1p-100f ? kv_inv_of(am) : 0.f;  // a smaller row counts as zeros: its reciprocal may be infinite
         hx = u32x2_t{pack_i16x2(kv_quant(x.x, inv), kv_quant(x.y, inv)), pack_i16x2(kv_quant(x.z, inv), kv_quant(x.w, inv))};
         hy = u32x2_t{pack_i16x2(kv_quant(y.x, inv), kv_quant(y.y, inv)), pack_i16x2(kv_quant(y.z, inv), kv_quant(y.w, inv))};
         if (u == 0) (kind == 1 ? a.map.kscale : a.map.vscale)[rowi] = kv_scale_of(am);

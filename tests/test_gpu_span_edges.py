@@ -136,3 +136,18 @@ def test_verify_drafts_long_paths(B, T, V, form, where):
     acc = _check_verify(t, None if form == "onehot" else d, drafts, u, 0.0 if form == "greedy" else 0.8, span=None if where == "middle" else [T - i % 2 * (T > 1) for i in range(B)])
     if T > 100:
         assert max(acc) > 192
+
+
+def test_append_of_rows_below_the_normal_numbers():
+    """A block-scaled row whose largest magnitude has no reciprocal within fp32: zeros stay zeros, the rest is off by at most that magnitude."""
+    B, T, Hq, Hkv, hd, S = 1, 4, 2, 2, 64, 16
+    cache = R.Cache(torch.ones(B, Hkv, S, hd), torch.ones(B, Hkv, S, hd), True)
+    g = torch.Generator().manual_seed(3)
+    x = _rnd(g, T, Hq + 2 * Hkv, hd).float()
+    x[:, :, ::3] = 0
+    x *= torch.tensor([1e-42, 1e-36, 3e-31, 1e-28])[:, None, None]
+    _ops().rope_append_at(x.view(T, -1).to(DEV), 1, 0, T, _i32([0]), _i32([4]), _table(64, 8), 1, 64, Hq, Hkv, hd, S, cache.rows[0], cache.rows[1], **cache.args())
+    v, want = cache.values(1)[0, :, 4:4 + T].transpose(0, 1), x[:, Hq + Hkv:].double()
+    top = want.abs().amax(-1, keepdim=True)
+    assert (v[want == 0] == 0).all()
+    assert ((v - want).abs() <= torch.where(top > 2.0 ** -100, 0.51 * top / 32767, top)).all()
