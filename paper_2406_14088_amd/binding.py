@@ -210,7 +210,8 @@ class _Fit:
         if _Fit.f32 is None:
             import torch
             _Fit.i32, _Fit.h16 = (torch.int32,), (torch.float16, torch.int16, torch.uint16)
-            _Fit.raw, _Fit.f32, _Fit.torch_c = (torch.uint8, torch.int64, torch.int32, torch.float32), (torch.float32,), torch._C
+            _Fit.raw, _Fit.torch_c = (torch.uint8, torch.int64, torch.int32, torch.float32), torch._C
+            _Fit.f32 = (torch.float32,)      # last: it stands for all of them
         self.where, self.dev = where, _Fit.torch_c._cuda_getDevice()
 
     def __call__(self, name: str, t, types, n: int):

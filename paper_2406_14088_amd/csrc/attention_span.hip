@@ -3,7 +3,8 @@
 // The T tokens of a sequence and the G = Hq / Hkv query heads of a kv head are R = T * G query rows that share every cache row: per tile
 // of 32 cache rows two matrix products,
 //     S^T[32 keys x 16 columns] = K[32 x hd] * Q^T[hd x 16],     O^T[hd x 16 columns] += V^T[hd x 32 keys] * P^T[32 x 16],
-// where q and the probabilities enter the matrix cores as two half terms, with about 22 significant bits, and K and V as stored.  Up to 8
+// where q and the probabilities enter the matrix cores as two half terms, and K and V as stored: about 22 significant bits for elements of the
+// scaled q from 2^-3 on (smaller ones to 2^-25) and for probabilities as said below.  Up to 8
 // query rows share the 16 columns with their low terms (columns c and c + 8: one product for both); with more a column is a row
 // and the low terms take a second product, which leaves the softmax without idle lanes (32 query rows on one wavefront: 77 us as four
 // tiles of 8, 71 as two of 16, at 3 x 8 tokens over 30011 rows, 32/8 heads).
@@ -29,11 +30,12 @@
 // W = 2 or 4 wavefronts share the rows of a sequence and join through LDS at the end; nsplit workgroups join in a second kernel.
 // Weights need the scores again once maximum and sum are final.  A workgroup with up to 16 query rows that has seen all rows and queries
 // of a kv head keeps them lane by lane, most of them in registers, and adds up the weights itself; else they go to the workspace and the
-// second kernel does.
+// second kernel does.  (The kernel of 16 query rows of 128 keeps 8 tiles at the price of up to 14 spilled registers over half rows, 3 over int16.)
 //
-// Measured, cold caches: 32 x 5 drafts over up to 1030 int16 rows, 32 heads of 128, 79 us (420 MB, 5.3 TB/s); 3 x 8 tokens over up to 30011
-// rows in pages of 64, 32/8 heads, 64 us (308 MB, 4.8 TB/s); 48 tokens with weights over up to 2111 rows, 64/8 heads, 77.6 us (321 MB,
-// 4.1 TB/s; 86 with all scores in the workspace, 67 without weights).  A kernel that only reads 300 MB takes 45 us.  A
+// Measured, cold caches: 32 x 5 drafts over up to 1030 int16 rows, 32 heads of 128, 77 us (420 MB, 5.5 TB/s); 3 x 8 tokens over up to 30011
+// rows in pages of 64, 32/8 heads, 61 us (308 MB, 5.0 TB/s); 48 tokens with weights over up to 2111 rows, 64/8 heads, 78 us (321 MB,
+// 4.1 TB/s; 86 with all scores in the workspace, 67 without weights); 8 x 512 tokens of a prompt over up to 4096 rows, 32/8 heads, 657 us
+// (int16: 1328), the cache read from L2 once per 32 query rows.  A kernel that only reads 300 MB takes 45 us.  A
 // workgroup's first tile arrives 5 to 10 us after the launch (lengths, page numbers and rows depend on each other while every compute
 // unit starts); the loop itself reads 7 TB/s.  Equal shares of all tiles for a fixed number of workgroups instead of whole items
 // balance lengths but leave nothing to overlap a workgroup's start and end with: 95 us for the drafts, 83 with weights.
@@ -73,7 +75,9 @@ __device__ __forceinline__ void span_split(u32x4_t n, f16x8_t *h, f16x8_t *l) {
     *l = __builtin_bit_cast(f16x8_t, low) - (_Float16)16.f;
 }
 
-// Query rows of a workgroup.
+// Query rows of a workgroup: the fewest that hold them all.  At 8 rows the kernels of 8 and of 16 take 78 and 80 us (32 x 5 over 1030 int16 rows),
+// 67.5 and 67.5 (48 over 2111 rows, 64/8 heads), with weights 78 and 97; at 16 rows the kernels of 16 and of 32 take 39.5 and 40.5 us (32 x 4 over 2000,
+// 32/8 heads), 71.5 and 73 (64 x 2, 64/8 heads), with weights 106 and 126.
 __host__ __device__ static inline int span_rows(int T, int G) {
     const int64_t R = (int64_t)T * G;
     return R <= 8 ? 8 : R <= 16 ? 16 : 32;

@@ -7,7 +7,7 @@
 // maximum of a block-scaled row is a reduction among them.
 //
 // Measured: 8 x 509 tokens, 32/8 heads of 128, paged, 40 us (185 MB, 4.6 TB/s; a copy of 4 GiB reaches 4.8); 32 x 5 tokens, 32 heads, four
-// partials, 7.8 us (37 MB, 4.7 TB/s).
+// partials, 8.0 us (37 MB, 4.6 TB/s).  Block-scaled rows take as long (39.7 and 39.1 us, 11.3 and 11.2 with the host's call).
 #include "kernels.h"
 
 template <bool SCALED>

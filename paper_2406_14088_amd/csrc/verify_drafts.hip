@@ -11,7 +11,8 @@
 // bound the reading of the rows (with a polynomial of degree 8 and no table, 15 of them): 4.9 TB/s, 6.3 TB/s for the maxima alone.
 //
 // Measured: 64 x 5 drafts, vocabulary 32000 (90 MB): 43 us, of it 22 for the rows, 5 for the decision, 7 for the weights of the rejected row
-// and 8 for the token, the last three a chain of dependent loads each; 128 x up to 7 drafts, vocabulary 128256: 138 us (rows 106, 9, 25, 10).
+// and 9 for the token, the last three a chain of dependent loads each; 128 x up to 7 drafts, vocabulary 128256: 130 to 156 us with the lengths drawn, at 156
+// rows 113, 10, 26, 10.  Drafts that were not sampled: 25 us for 64 x 5 of 32000, greedy 20.
 #include "kernels.h"
 
 #define VD_THREADS 256
