@@ -230,8 +230,9 @@ int rl_op_logprob_gather(const float *logits, int64_t ld, int32_t M, int32_t V, 
  * not checked; page_size a power of two in [16, 4096], table_stride * page_size >= S); NULL: slabs [B][Hkv][S][hd], page_size and
  * table_stride without effect.  hd is 64 or 128.  weight (fp32) and row_pos / pos (int32) are [B][Hkv][S] arrays beside the cache,
  * indexed by slot whether the cache is paged or not.  Device pointers of q, out, kc, vc and qkv are 16-byte aligned (E_SHAPE
- * otherwise), all others by their element.  A batch that would need 2^32 threads or more in a launch is refused with E_SHAPE (256 per
- * appended token, 512 or 1024 per kv head to evict from, 256 per 8192 logits of a row to verify, 128 per split and 8 to 32 query rows of a kv head). */
+ * otherwise), all others by their element.  A batch that would need 2^32 threads or more in a
+ * launch is refused with E_SHAPE (256 per appended token, 512 or 1024 per kv head to evict from, 256 per 8192 logits of a row to
+ * verify, 128 per split and 8 to 32 query rows of a kv head). */
 
 /* Rotary table with the frequencies scaled for contexts longer than the model was trained on: tab fp32 [n_pos, rot_dim/2, 2] =
  * (cos, sin) of pos * f_r, f_r evaluated in fp64 on the host and copied (synchronously).  rot_dim is the number of leading head
@@ -252,8 +253,9 @@ int rl_op_build_rope_table_scaled(float *tab, int32_t n_pos, int32_t rot_dim, fl
  * style 0 turns elements (2r, 2r+1), style 1 elements (r, r + rot_dim/2); the others are copied.  rot_dim % 8 == 0, 8 <= rot_dim <= hd.
  * q goes to q_f32 and / or q_f16 (+ q_f16_lo, its second half term), each [B*T, Hq*hd] or NULL; k and v become cache rows.
  * weight and row_pos (either may be NULL): the entry of every new row is set to 0 and to its position.
- * A row whose position is outside [0, tab_rows) or whose slot is outside [0, S) is skipped whole.  Halves saturate at +-65504, a NaN stays one;
- * a block-scaled row that holds one gets a scale that is NaN, one whose largest magnitude is not above 2^-100 becomes zeros. */
+ * A row whose position is outside [0, tab_rows) or whose slot is outside [0, S) is skipped whole.  Halves saturate at +-65504, a
+ * NaN stays one; a block-scaled row that holds one gets a scale that is NaN, one whose largest magnitude is not above 2^-100 becomes
+ * zeros. */
 int rl_op_rope_append_at(const float *qkv, int32_t nsplit, size_t split_stride, int32_t B, int32_t T, const int32_t *d_pos,
                          const int32_t *d_slot, const int32_t *d_span, const float *rope_tab, int32_t tab_rows, int32_t rope_style,
                          int32_t rot_dim, int32_t Hq, int32_t Hkv, int32_t hd, int32_t S, float *q_f32, uint16_t *q_f16, uint16_t *q_f16_lo,
@@ -267,13 +269,14 @@ int rl_op_rope_append_at(const float *qkv, int32_t nsplit, size_t split_stride, 
  * weight (or NULL): weight[b, h, j] += the sum of p_j over the queries of kv head h and the span's valid tokens -- what
  * rl_op_evict_rows goes by.  Sums are formed in a fixed order (the same bits every time), also those of weight.
  * nsplit: workgroups that share the rows of a sequence, 1 .. 64, or 0: chosen from the shape.  ws: fp32 workspace of ws_floats
- * elements, 16-byte aligned.  rl_op_span_attention_ws_floats(same arguments, weights = whether weight is given) are enough for this B and T and every
- * smaller one, so that a program may size it once for its largest step; a call whose own need is above ws_floats returns RL_GEN_E_CAPACITY
- * (ws may be NULL for one that needs nothing).  The weights' scores take 4 B T Hq S bytes of it where T Hq / Hkv is a multiple of 32.
- * A query that holds a NaN or an infinity, or sees a row whose K or V holds a NaN, gives NaN in out and out_lo (from q or K: also in weight); a block-scaled row counts as one
- * whose scale is not finite.  An infinite half in V gives NaN or the largest half of its sign, one in K a score that is infinite or NaN.  Rows that a
- * query does not see never reach its result, whatever they hold.  Finite q times log2(e) / sqrt(hd) saturates at +-131008, out and out_lo at
- * +-65504.  Hq/Hkv <= 64. */
+ * elements, 16-byte aligned.  rl_op_span_attention_ws_floats(same arguments, weights = whether weight is given) are enough for
+ * this B and T and every smaller one, so that a program may size it once for its largest step; a call whose own need is above
+ * ws_floats returns RL_GEN_E_CAPACITY (ws may be NULL for one that needs nothing).  The weights' scores take 4 B T Hq S bytes of it
+ * where T Hq / Hkv is a multiple of 32.
+ * A query that holds a NaN or an infinity, or sees a row whose K or V holds a NaN, gives NaN in out and out_lo (from q or K: also in
+ * weight); a block-scaled row whose scale is not finite counts as one that holds a NaN.  An infinite half in V gives NaN or the
+ * largest half of its sign, one in K a score that is infinite or NaN.  Rows that a query does not see never reach its result,
+ * whatever they hold.  Finite q times log2(e) / sqrt(hd) saturates at +-131008, out and out_lo at +-65504.  Hq/Hkv <= 64. */
 int rl_op_span_attention(const float *q, const uint16_t *kc, const uint16_t *vc, const float *kscale, const float *vscale,
                          const int32_t *table, int32_t table_stride, int32_t page_size, const int32_t *d_len, const int32_t *d_span,
                          uint16_t *out, uint16_t *out_lo, float *weight, float *ws, size_t ws_floats, int32_t B, int32_t T, int32_t Hq,
@@ -313,8 +316,8 @@ size_t rl_op_evict_rows_ws_bytes(int32_t B, int32_t Hkv, int32_t S, int32_t keep
  * NaN where that row's largest logit is not finite), 0 for -1.
  * Weights and sums are formed in fp64 from the fp32 logits (relative error below 1e-11), in a fixed order.  1 <= T <= 256,
  * 1 <= V <= 2^30.
- * ws: DEVICE, ws_bytes long, 8-byte aligned.  rl_op_verify_drafts_ws_bytes are enough for this B and T and every smaller one; a call whose own need
- * is above ws_bytes returns RL_GEN_E_CAPACITY. */
+ * ws: DEVICE, ws_bytes long, 8-byte aligned.  rl_op_verify_drafts_ws_bytes are enough for this B and T and every smaller one; a call
+ * whose own need is above ws_bytes returns RL_GEN_E_CAPACITY. */
 int rl_op_verify_drafts(const float *target, int64_t ldt, const float *draft, int64_t ldd, const int32_t *drafts, const float *u,
                         const int32_t *d_span, int32_t B, int32_t T, int32_t V, double temperature, int32_t *accepted, int32_t *tokens,
                         float *logp, void *ws, size_t ws_bytes, void *hip_stream);

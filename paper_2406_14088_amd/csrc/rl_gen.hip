@@ -1758,7 +1758,8 @@ int rl_op_rope_append_at(const float *qkv, int32_t nsplit, size_t split_stride, 
     if (!qkv || !d_pos || !d_slot || !rope_tab || (q_f16_lo && !q_f16)) return RL_GEN_E_NULL;
     RopeAppendAtArgs a;
     if (int rc = span_cache_map(kc, vc, kscale, vscale, table, table_stride, page_size, B, Hkv, hd, S, &a.map)) return rc;
-    if (nsplit < 1 || split_stride % 4 || (nsplit > 1 && split_stride > (size_t)PTRDIFF_MAX / sizeof(float) / nsplit) || T <= 0 || !grid_fits((int64_t)B * T, 256) || tab_rows <= 0 || (rope_style != 0 && rope_style != 1) ||
+    if (nsplit < 1 || split_stride % 4 || (nsplit > 1 && split_stride > (size_t)PTRDIFF_MAX / sizeof(float) / nsplit)) return RL_GEN_E_SHAPE;
+    if (T <= 0 || !grid_fits((int64_t)B * T, 256) || tab_rows <= 0 || (rope_style != 0 && rope_style != 1) ||
         rot_dim < 8 || rot_dim > hd || rot_dim % 8 || Hq <= 0 || (int64_t)Hq + 2 * (int64_t)Hkv > 65535)
         return RL_GEN_E_SHAPE;
     if (((uintptr_t)qkv | (uintptr_t)q_f32 | (uintptr_t)q_f16 | (uintptr_t)q_f16_lo | (uintptr_t)rope_tab) % 16) return RL_GEN_E_SHAPE;
