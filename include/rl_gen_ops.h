@@ -276,7 +276,8 @@ int rl_op_rope_append_at(const float *qkv, int32_t nsplit, size_t split_stride, 
  * A query that holds a NaN or an infinity, or sees a row whose K or V holds a NaN, gives NaN in out and out_lo (from q or K: also in
  * weight); a block-scaled row whose scale is not finite counts as one that holds a NaN.  An infinite half in V gives NaN or the
  * largest half of its sign, one in K a score that is infinite or NaN.  Rows that a query does not see never reach its result,
- * whatever they hold.  Finite q times log2(e) / sqrt(hd) saturates at +-131008, out and out_lo at +-65504.  Hq/Hkv <= 64. */
+ * whatever they hold.  Finite q times log2(e) / sqrt(hd) is taken to 2^-22 of itself, below 2^-3 to 2^-25, and saturates at +-131008;
+ * out and out_lo saturate at +-65504.  Hq/Hkv <= 64. */
 int rl_op_span_attention(const float *q, const uint16_t *kc, const uint16_t *vc, const float *kscale, const float *vscale,
                          const int32_t *table, int32_t table_stride, int32_t page_size, const int32_t *d_len, const int32_t *d_span,
                          uint16_t *out, uint16_t *out_lo, float *weight, float *ws, size_t ws_floats, int32_t B, int32_t T, int32_t Hq,
